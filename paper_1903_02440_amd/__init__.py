@@ -555,3 +555,5 @@ def spk_count_events_strided(wave, Cout, K, stride, pad, count=None, stream=None
 
 
 INF = math.inf
+
+from .readout import *  # noqa: E402,F401,F403  (the readout operators, from libspyke_readout.h)

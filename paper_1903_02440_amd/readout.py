@@ -1,0 +1,153 @@
+"""Binding of the readout operators (``include/libspyke_readout.h``): the gated
+delta rule, its single-sample form, and winners drawn from scores.
+
+The functions have the names of the C entry points and, as those of the package,
+only marshal: dtype and shape checks, outputs and workspaces that are not given,
+raw pointers and the stream.  The call runs on the tensors' device, on its
+current stream unless one is given.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import _F, _I, _P, _Z, _check, _lib, _need, _out, _ptr, _stream, _ws
+
+_SIGS = {
+    "spk_delta_rule_workspace_size": (_Z, [_I] * 7),
+    "spk_delta_rule": (_I, [_P] * 5 + [_I] * 7 + [_F] + [_P] * 5 + [_Z, _P]),
+    "spk_delta_rule_step": (_I, [_P] * 5 + [_I] * 6 + [_F] + [_P] * 3),
+    "spk_sample_winners_workspace_size": (_Z, [_I] * 5),
+    "spk_sample_winners": (_I, [_P, _I, _P, _P] + [_I] * 5 + [_F, _I, _F, _F] + [_P] * 3 + [_Z, _P]),
+}
+for _name, (_res, _args) in _SIGS.items():
+    _fn = getattr(_lib, _name)
+    _fn.restype = _res
+    _fn.argtypes = _args
+
+SPK_F32, SPK_BF16 = 0, 1
+_DTYPES = {torch.float32: SPK_F32, torch.bfloat16: SPK_BF16}
+
+__all__ = ["SPK_F32", "SPK_BF16"] + list(_SIGS)
+
+
+def _dtype(t, name):
+    if t.dtype not in _DTYPES:
+        raise TypeError(f"{name}: expected torch.float32 or torch.bfloat16, got {t.dtype}")
+    return _DTYPES[t.dtype]
+
+
+def _same_device(dev, **tensors):
+    for name, t in tensors.items():
+        if isinstance(t, torch.Tensor) and t.device != dev:
+            raise ValueError(f"{name}: on {t.device}, the call's tensors are on {dev}")
+
+
+def _on(dev, stream, call):
+    """call(stream pointer) with `dev` current (a launch goes to the current device)."""
+    with torch.cuda.device(dev):
+        _check(call(_stream(stream)))
+
+
+# ---------------------------------------------------------------- delta rule
+def spk_delta_rule_workspace_size(dtype, B, L, Hk, Hv, dk, dv) -> int:
+    return int(_lib.spk_delta_rule_workspace_size(dtype, B, L, Hk, Hv, dk, dv))
+
+
+def _delta_args(q, k, v, g, beta, lengths, initial_state):
+    """Checks the inputs of a batch call; (dtype code, B, L, Hk, Hv, dk, dv)."""
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        if t.dim() != 4:
+            raise ValueError(f"{name}: expected [B, L, heads, size], got shape {tuple(t.shape)}")
+    dt = _dtype(q, "q")
+    B, L, Hk, dk = q.shape
+    Hv, dv = v.shape[2:]
+    _need(q, q.dtype, (B, L, Hk, dk), "q")
+    _need(k, q.dtype, (B, L, Hk, dk), "k")
+    _need(v, q.dtype, (B, L, Hv, dv), "v")
+    _need(g, torch.float32, (B, L, Hv), "g")
+    _need(beta, torch.float32, (B, L, Hv), "beta")
+    if lengths is not None:
+        _need(lengths, torch.int32, (B,), "lengths")
+    if initial_state is not None:
+        _need(initial_state, torch.float32, (B, Hv, dk, dv), "initial_state")
+    return dt, B, L, Hk, Hv, dk, dv
+
+
+def _rows(t, like, dtype, lengths, name):
+    """An output of rows per sample; a new one is 0 behind the sequences' lengths."""
+    if t is None and lengths is not None:
+        return torch.zeros(like.shape, dtype=dtype, device=like.device)
+    return _out(t, like.shape, dtype, like.device, name)
+
+
+def spk_delta_rule(q, k, v, g, beta, scale=1.0, initial_state=None, lengths=None, out=None, final_state=None,
+                   workspace=None, stream=None):
+    """Gated delta rule over a batch of sequences: q, k [B,L,Hk,dk] and v [B,L,Hv,dv] of one dtype (float32 or
+    bfloat16), g, beta f32 [B,L,Hv] -> (out [B,L,Hv,dv], final_state f32 [B,Hv,dk,dv] or None).  lengths i32 [B]
+    gives each sequence's samples; rows of a given `out` behind them are left as they were, those of a new one
+    are 0.  final_state may be initial_state."""
+    dt, B, L, Hk, Hv, dk, dv = _delta_args(q, k, v, g, beta, lengths, initial_state)
+    dev = q.device
+    out = _rows(out, v, q.dtype, lengths, "out")
+    final_state = _out(final_state, (B, Hv, dk, dv), torch.float32, dev, "final_state")
+    n = spk_delta_rule_workspace_size(dt, B, L, Hk, Hv, dk, dv)
+    ws = _ws(workspace, n, dev)
+    _same_device(dev, k=k, v=v, g=g, beta=beta, lengths=lengths, initial_state=initial_state, out=out,
+                 final_state=final_state, workspace=ws)
+    _on(dev, stream, lambda st: _lib.spk_delta_rule(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), dt, B, L, Hk, Hv, dk, dv, float(scale), _ptr(lengths),
+        _ptr(initial_state), _ptr(out), _ptr(final_state), _ptr(ws), n, st))
+    return out, (final_state if final_state is not False else None)
+
+
+def spk_delta_rule_step(q, k, v, g, beta, state, scale=1.0, out=None, stream=None):
+    """One sample of every sequence: q, k [B,Hk,dk], v [B,Hv,dv], g, beta f32 [B,Hv]; state f32 [B,Hv,dk,dv] is
+    updated in place -> out [B,Hv,dv]."""
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        if t.dim() != 3:
+            raise ValueError(f"{name}: expected [B, heads, size], got shape {tuple(t.shape)}")
+    dt = _dtype(q, "q")
+    B, Hk, dk = q.shape
+    Hv, dv = v.shape[1:]
+    _need(q, q.dtype, (B, Hk, dk), "q")
+    _need(k, q.dtype, (B, Hk, dk), "k")
+    _need(v, q.dtype, (B, Hv, dv), "v")
+    _need(g, torch.float32, (B, Hv), "g")
+    _need(beta, torch.float32, (B, Hv), "beta")
+    _need(state, torch.float32, (B, Hv, dk, dv), "state")
+    out = _out(out, (B, Hv, dv), q.dtype, q.device, "out")
+    _same_device(q.device, k=k, v=v, g=g, beta=beta, state=state, out=out)
+    _on(q.device, stream, lambda st: _lib.spk_delta_rule_step(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), dt, B, Hk, Hv, dk, dv, float(scale), _ptr(state), _ptr(out),
+        st))
+    return out
+
+
+# ---------------------------------------------------------------- drawing
+def spk_sample_winners_workspace_size(dtype, B, C, H, W) -> int:
+    return int(_lib.spk_sample_winners_workspace_size(dtype, B, C, H, W))
+
+
+def spk_sample_winners(scores, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, t_first=None, T=1, winners=None,
+                       n_winners=None, workspace=None, stream=None):
+    """One winner per image drawn from scores (float32 or bfloat16) [B,C,H,W] with u f32 [B] in [0, 1) ->
+    (winners i32 [B,1,4] = (f,t,y,x), n_winners i32 [B]).  t_first u8 [B,C,H,W] masks the silent neurons
+    (t_first >= T)."""
+    if scores.dim() != 4:
+        raise ValueError(f"scores: expected [B, C, H, W], got shape {tuple(scores.shape)}")
+    dt = _dtype(scores, "scores")
+    B, C, H, W = scores.shape
+    dev = scores.device
+    _need(scores, scores.dtype, (B, C, H, W), "scores")
+    _need(u, torch.float32, (B,), "u")
+    if t_first is not None:
+        _need(t_first, torch.uint8, (B, C, H, W), "t_first")
+    winners = _out(winners, (B, 1, 4), torch.int32, dev, "winners")
+    n_winners = _out(n_winners, (B,), torch.int32, dev, "n_winners")
+    n = spk_sample_winners_workspace_size(dt, B, C, H, W)
+    ws = _ws(workspace, n, dev)
+    _same_device(dev, u=u, t_first=t_first, winners=winners, n_winners=n_winners, workspace=ws)
+    _on(dev, stream, lambda st: _lib.spk_sample_winners(
+        _ptr(scores), dt, _ptr(t_first), _ptr(u), B, int(T), C, H, W, float(temperature), int(top_k), float(top_p),
+        float(min_p), _ptr(winners), _ptr(n_winners), _ptr(ws), n, st))
+    return winners, n_winners
