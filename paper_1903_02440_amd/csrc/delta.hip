@@ -20,7 +20,7 @@ int check(const Args &a, const char *name) {
     SPK_REQUIRE(a.Hv % a.Hk == 0, SPK_E_SHAPE, "%s: Hv=%d is not a multiple of Hk=%d", name, a.Hv, a.Hk);
     SPK_REQUIRE(a.dk <= 256, SPK_E_RANGE, "%s: dk=%d > 256", name, a.dk);
     SPK_REQUIRE(a.dv <= 4096, SPK_E_RANGE, "%s: dv=%d > 4096", name, a.dv);
-    SPK_REQUIRE((int64_t)a.B * a.Hv <= 65536, SPK_E_RANGE, "%s: B*Hv above 65536", name);
+    SPK_REQUIRE((int64_t)a.B * a.Hv <= 65535, SPK_E_RANGE, "%s: B*Hv above 65535", name);
     SPK_REQUIRE(a.L <= (1 << 24), SPK_E_RANGE, "%s: L=%d > 2^24", name, a.L);
     SPK_REQUIRE(std::isfinite(a.scale), SPK_E_ARG, "%s: scale must be finite", name);
     return SPK_OK;
@@ -163,11 +163,14 @@ void launch_seq(const void *q, const void *k, const void *v, const float *g, con
 #undef SPK_SEQ
 }
 
+// A call of more samples goes in chunks.
+bool in_chunks(const Args &a) { return a.L > 8; }
+
 }  // namespace
 
 extern "C" size_t spk_delta_rule_workspace_size(int dtype, int B, int L, int Hk, int Hv, int dk, int dv) {
-    (void)dtype, (void)B, (void)L, (void)Hk, (void)Hv, (void)dk, (void)dv;
-    return 0;
+    const Args a{dtype, B, L, Hk, Hv, dk, dv, 1.0f};
+    return check(a, "") == SPK_OK && in_chunks(a) ? chunk_workspace(a) : 0;
 }
 
 extern "C" int spk_delta_rule(const void *q, const void *k, const void *v, const float *g, const float *beta, int dtype,
@@ -181,8 +184,13 @@ extern "C" int spk_delta_rule(const void *q, const void *k, const void *v, const
     SPK_REQUIRE((q && k && v && g && beta && out) || L == 0, SPK_E_ARG, "%s: q, k, v, g, beta and out are required",
                 name);
     if (L == 0 && !final_state) return spk::ok();
-    (void)workspace, (void)ws_bytes;
     hipStream_t st = spk::as_stream(stream);
+    if (in_chunks(a)) {
+        const size_t need = chunk_workspace(a);
+        SPK_REQUIRE(workspace && ws_bytes >= need, SPK_E_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", name,
+                    workspace ? ws_bytes : (size_t)0, need);
+        return chunk_forward(q, k, v, g, beta, a, lengths, initial_state, out, final_state, workspace, st, name);
+    }
     if (dtype == SPK_F32) launch_seq<float>(q, k, v, g, beta, a, lengths, initial_state, out, final_state, st);
     else launch_seq<uint16_t>(q, k, v, g, beta, a, lengths, initial_state, out, final_state, st);
     return spk::check_launch(name);

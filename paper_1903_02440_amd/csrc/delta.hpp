@@ -15,6 +15,12 @@ struct Args {
 // Sizes and flags of a call; SPK_OK or the recorded error.
 int check(const Args &a, const char *name);
 
+// The batch call over chunks of samples, and the bytes of its workspace.
+size_t chunk_workspace(const Args &a);
+int chunk_forward(const void *q, const void *k, const void *v, const float *g, const float *beta, const Args &a,
+                  const int32_t *lengths, const float *state_in, void *out, float *state_out, void *ws, hipStream_t st,
+                  const char *name);
+
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 // bfloat16 elements are carried as uint16_t.

@@ -1,0 +1,157 @@
+// The gated delta rule over chunks of C samples: what its kernels share.
+//
+// Within a chunk that a state S enters, with gamma the running sum of the log
+// decays, E_i = e^{gamma_i}, D_ij = e^{gamma_i - gamma_j} (j <= i), and
+// last_i = e^{gamma_C - gamma_i}:
+//     (I + A) U = beta (V - E K S)      A_ij = beta_i D_ij k_i . k_j  (j < i)
+//     out       = scale (E Q S + P U)   P_ij = D_ij q_i . k_j         (j <= i)
+//     S        <- E_C S + K^T (last U)
+// T = (I + A)^-1, P and the decays depend on the inputs alone, so all chunks
+// make them at once; the states then go through the chunks in order.
+//
+// Products run on the 16-bit matrix cores with float sums.  A float operand is
+// the exact sum of three bfloat16 terms (8 bits each), a bfloat16 input is one;
+// of a product of two such sums the terms below 2^-24 of the first are left
+// out.  Against the float matrix cores (1/16 of the rate) three or six products
+// of terms cost 3/16 to 6/16, at the same precision.
+//
+// Operands lie in fragments: for 16 rows and 32 summed indices the 16 bytes of
+// each lane in turn (1 KiB a term).  The result of a matrix instruction holds,
+// in lane (n, g), rows 4g..4g+3 of column n; taking two result tiles as one
+// right operand gives lane group g the indices 4g..4g+3 and 16+4g..16+4g+3 of
+// the 32.  Fragments are laid out for that order, so results feed the next
+// product without leaving their lane.
+#pragma once
+
+#include "delta.hpp"
+
+namespace spk {
+namespace delta {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int FRAG = 1024;  // bytes of one term of a fragment
+
+// index within a group of 32 of element j of lane group g
+__device__ __forceinline__ int slot(int g, int j) { return j < 4 ? 4 * g + j : 12 + 4 * g + j; }
+
+template <int N>
+struct Terms {
+    u32x4 t[N];
+};
+
+// The upper halves of two floats as one word.
+__device__ __forceinline__ uint32_t upper2(uint32_t lo, uint32_t hi) {
+    return __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+}
+
+// Eight floats as N bfloat16 terms.  Each term takes the leading 8 bits of what
+// is left (truncated, so that the remainder is exact): three hold every float.
+// The last term of a shorter sum is rounded to nearest.
+template <int N>
+__device__ __forceinline__ Terms<N> split(const float (&x)[8]) {
+    Terms<N> r;
+    float y[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = x[j];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (i == N - 1 && N < 3) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                r.t[i][j] = (uint32_t)from_float<uint16_t>(y[2 * j]) |
+                            ((uint32_t)from_float<uint16_t>(y[2 * j + 1]) << 16);
+            break;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            r.t[i][j] = upper2(__float_as_uint(y[2 * j]), __float_as_uint(y[2 * j + 1]));
+        if (i < N - 1) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] -= __uint_as_float(__float_as_uint(y[j]) & 0xFFFF0000u);
+        }
+    }
+    return r;
+}
+template <int N>
+__device__ __forceinline__ Terms<N> split(const f32x4 &a, const f32x4 &b) {
+    const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    return split<N>(x);
+}
+
+__device__ __forceinline__ f32x4 mfma(const u32x4 &a, const u32x4 &b, const f32x4 &c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
+                                                   0, 0);
+}
+
+// c += a b, smaller products of terms first.
+template <int NA, int NB>
+__device__ __forceinline__ void mma(f32x4 &c, const Terms<NA> &a, const Terms<NB> &b) {
+    constexpr int M = NA > NB ? NA : NB;
+#pragma unroll
+    for (int o = M - 1; o >= 0; --o)
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+            if (o - i >= 0 && o - i < NB) c = mfma(a.t[i], b.t[o - i], c);
+}
+
+// The lane's part of a fragment of N terms.
+template <int N>
+__device__ __forceinline__ Terms<N> frag(const char *p, int lane) {
+    Terms<N> r;
+#pragma unroll
+    for (int i = 0; i < N; ++i) r.t[i] = *reinterpret_cast<const u32x4 *>(p + i * FRAG + lane * 16);
+    return r;
+}
+template <int N>
+__device__ __forceinline__ void put_frag(char *p, int lane, const Terms<N> &x) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4 *>(p + i * FRAG + lane * 16) = x.t[i];
+}
+
+// Sizes of a chunk's operands.  DS: groups of 32 of dk; MT: tiles of 16
+// samples.  Float inputs take chunks of 32 samples, so that their three terms
+// fit the LDS at dk = 256; bfloat16 ones take 64.
+template <class E>
+struct Type;
+template <>
+struct Type<float> {
+    static constexpr int NT = 3, MT = 2, NP = 3;
+};
+template <>
+struct Type<uint16_t> {
+    // the products that only reach a bfloat16 output take two terms (2^-17)
+    static constexpr int NT = 1, MT = 4, NP = 2;
+};
+template <class E, int DS>
+struct Lay {
+    static constexpr int NT = Type<E>::NT, MT = Type<E>::MT, NP = Type<E>::NP;
+    static constexpr int C = 16 * MT, GP = MT / 2;
+    // a triangular C x C operand: the fragments that are not zero throughout
+    static constexpr int TRI = MT == 4 ? 6 : 2;
+    static constexpr int K = MT * DS * NT * FRAG;  // rows of K (or Q), summed over dk: [mt][s][term]
+    static constexpr int KT = 2 * DS * GP * NT * FRAG;  // its transpose, summed over the samples: [t][gp][term]
+    static constexpr int COEF = FRAG;              // E, beta, last: f32 [3][C]
+    // fragment (mt, gp <= mt / 2) of a lower triangular operand
+    static __host__ __device__ constexpr int lower(int mt, int gp) { return mt < 2 ? mt : 2 * mt - 2 + gp; }
+};
+
+constexpr int chunk_of(int dtype) { return dtype == SPK_F32 ? 32 : 64; }
+
+// e^g for sums of log decays: -inf (all forgotten) as a number whose
+// exponential is 0, so that differences of sums stay defined.
+__device__ __forceinline__ double log_decay(float g) { return g < -1e4f ? -1e4 : (double)g; }
+
+// Copies n bytes (a multiple of 1 KiB) to LDS, past the registers; both ends
+// 16-byte aligned.  All waves of the workgroup take part; wait for vmcnt(0)
+// and a barrier before use.
+__device__ __forceinline__ void to_lds(char *dst, const char *src, int n, int wave, int waves, int lane) {
+    for (int o = wave * FRAG; o < n; o += waves * FRAG)
+        __builtin_amdgcn_global_load_lds(reinterpret_cast<const u32x4 *>(src + o) + lane,
+                                         reinterpret_cast<u32x4 *>(dst + o), 16, 0, 0);
+}
+
+}  // namespace delta
+}  // namespace spk
