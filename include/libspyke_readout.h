@@ -66,6 +66,27 @@ SPK_API int spk_delta_rule_step(const void *q, const void *k, const void *v, con
                                 int dtype, int B, int Hk, int Hv, int dk, int dv, float scale, float *state, void *out,
                                 void *stream);
 
+/* Gradients of spk_delta_rule's (out, final_state) with respect to all its
+ * inputs, for rates, decays, keys and values that are themselves learnt.
+ *   d_out          dtype [B][L][Hv][dv].
+ *   d_final_state  f32 [B][Hv][dk][dv] or NULL (zeros).
+ *   d_q, d_k       dtype [B][L][Hk][dk], summed over the value heads of a
+ *                  key head; d_v dtype [B][L][Hv][dv]; d_g, d_beta
+ *                  f32 [B][L][Hv]; all required.
+ *   d_initial_state f32 [B][Hv][dk][dv] or NULL (not wanted); may be
+ *                  d_final_state.
+ * The other arguments are those of the forward call; its states are computed
+ * again.  Rows behind a sequence's length are neither read nor written.
+ * Repeated calls give the same bits.  Limits as spk_delta_rule.
+ * Workspace: spk_delta_rule_backward_workspace_size(...) bytes.             */
+SPK_API size_t spk_delta_rule_backward_workspace_size(int dtype, int B, int L, int Hk, int Hv, int dk, int dv);
+SPK_API int spk_delta_rule_backward(const void *q, const void *k, const void *v, const float *g, const float *beta,
+                                    int dtype, int B, int L, int Hk, int Hv, int dk, int dv, float scale,
+                                    const int32_t *lengths, const float *initial_state, const void *d_out,
+                                    const float *d_final_state, void *d_q, void *d_k, void *d_v, float *d_g,
+                                    float *d_beta, float *d_initial_state, void *workspace, size_t ws_bytes,
+                                    void *stream);
+
 /* ------------------------------------------------------------------------
  * One winner per image drawn from its neurons' scores (spk_kwta with k = 1
  * takes the largest; exploration under a reward draws instead).  Among an

@@ -1,0 +1,559 @@
+// Gradients of the gated delta rule over chunks of samples (gfx950).
+//
+// With dO the gradient of out and dS that of the state that leaves a chunk, S
+// the one that entered it (the other names as in delta_chunk.hpp):
+//     dU  = scale P^T dO + last (K dS)       Y = T^T dU
+//     dS <- E_C dS + scale Q^T (E dO) - K^T (beta E Y)
+// goes from the last chunk to the first, column by column of dv like the
+// states.  What is left needs no order, so all chunks do it at once; with
+// M = Y U^T (j < i) and N = scale dO U^T (j <= i), both weighed by D:
+//     dv    = beta Y
+//     dq    = scale E (dO S^T) + N K
+//     r     = -E (Y S^T) - M K               the rows of keys, beta apart
+//     c     = last (U dS^T) + N^T Q - (beta M)^T K   their columns
+//     dk    = beta r + c
+//     dbeta_i  = y_i . v_i + k_i . r_i
+//     dgamma_i = q_i . dq_i + beta_i k_i . r_i - k_i . c_i, and <dS, S_C> at the end,
+// since gamma_i scales q_i and k_i's row by e^gamma_i and k_i's column by its
+// inverse; dg is the sum of dgamma from i on.  <dS, S_C> = E_C <dS, S> plus the
+// sum of k_j . (last U dS^T)_j.
+#include <algorithm>
+
+#include "delta_kernels.hpp"
+
+namespace spk {
+namespace delta {
+
+// Grid and columns as the states' kernel (delta_kernels.hpp), chunks from last
+// to first; a wave carries 16 columns of dS.
+template <class E, int DS, int NBUF>
+__global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out, Args a,
+                                                     const int32_t *__restrict__ lengths, int compute, Chunks w,
+                                                     Kept kept, const float *d_last, float *d_first) {
+    using F = Blob<E, DS, true>;
+    constexpr int C = F::C, MT = F::MT, NT = F::NT, GP = F::GP;
+    constexpr int HEADP = F::HEAD - F::T, ONE = F::KEY + HEADP;  // coefficients, T^T, P^T
+    extern __shared__ char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, gr = lane >> 4;
+    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+    const int b = blockIdx.x / a.Hv, h = blockIdx.x % a.Hv, hk = h / (a.Hv / a.Hk);
+    const int n = lengths ? max(0, min(a.L, lengths[b])) : a.L, nc = (n + C - 1) / C;
+    const int col = ((int)blockIdx.y * compute + wv) * 16 + m;
+    const bool mine = wv < compute && col - m < kept.dvp, live = mine && col < a.dv;
+    const int64_t s0 = (int64_t)blockIdx.x * a.dk * a.dv + col;
+    const char *key = w.key + ((int64_t)b * a.Hk + hk) * w.NC * F::KEY;
+    const char *head = w.head + (int64_t)blockIdx.x * w.NC * F::HEAD + F::T;
+    f32x4 S[2 * DS];
+#pragma unroll
+    for (int t = 0; t < 2 * DS; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int d = 16 * t + 4 * gr + r;
+            S[t][r] = live && d < a.dk && d_last ? d_last[s0 + (int64_t)d * a.dv] : 0.0f;
+        }
+    auto fetch = [&](int c) {
+        char *dst = lds + (c % NBUF) * ONE;
+        to_lds(dst, key + (int64_t)c * F::KEY, F::KEY, wv, waves, lane);
+        to_lds(dst + F::KEY, head + (int64_t)c * F::HEAD, HEADP, wv, waves, lane);
+    };
+    const int64_t vstep = (int64_t)a.Hv * a.dv;
+    const int64_t v0 = ((int64_t)b * a.L * a.Hv + h) * a.dv + col;
+    if (NBUF == 2 && nc) fetch(nc - 1);
+    for (int c = nc - 1; c >= 0; --c) {
+        if (NBUF == 1) {
+            if (c < nc - 1) __syncthreads();
+            fetch(c);
+        }
+        float o[MT][4];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = c * C + 16 * mt + 4 * gr + r;
+                o[mt][r] = live && i < n ? to_float(d_out[v0 + i * vstep]) : 0.0f;
+            }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (NBUF == 2 && c > 0) fetch(c - 1);
+        if (!mine) continue;
+        const char *K = lds + (c % NBUF) * ONE, *KT = K + F::K, *QT = KT + F::KT, *H = K + F::KEY;
+        const char *TT = H + (F::TTAT - F::T), *PT = H + (F::PAT - F::T);
+        const float *co = reinterpret_cast<const float *>(H);
+        float *dst = kept.dS + ((int64_t)blockIdx.x * w.NC + c) * 32 * DS * kept.dvp + col;
+#pragma unroll
+        for (int t = 0; t < 2 * DS; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) dst[(int64_t)(16 * t + 4 * gr + r) * kept.dvp] = S[t][r];
+        f32x4 X[MT], Z[MT], Y[MT];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) X[mt] = Z[mt] = Y[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < DS; ++s) {
+            const Terms<3> st = split<3>(S[2 * s], S[2 * s + 1]);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) mma<NT, 3>(X[mt], frag<NT>(K + (mt * DS + s) * NT * FRAG, lane), st);
+        }
+#pragma unroll
+        for (int gp = 0; gp < GP; ++gp) {
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = o[2 * gp + (j >> 2)][j & 3];
+            const Terms<NT> ot = split<NT>(x);
+#pragma unroll
+            for (int mt = 0; mt <= 2 * gp + 1; ++mt) mma<3, NT>(Z[mt], frag<3>(PT + F::upper(mt, gp) * 3 * FRAG, lane), ot);
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            const f32x4 la = *reinterpret_cast<const f32x4 *>(co + 2 * C + 16 * mt + 4 * gr);
+            X[mt] = la * X[mt] + a.scale * Z[mt];  // dU
+        }
+#pragma unroll
+        for (int gp = 0; gp < GP; ++gp) {
+            const Terms<3> ut = split<3>(X[2 * gp], X[2 * gp + 1]);
+#pragma unroll
+            for (int mt = 0; mt <= 2 * gp + 1; ++mt) mma<3, 3>(Y[mt], frag<3>(TT + F::upper(mt, gp) * 3 * FRAG, lane), ut);
+        }
+        float *yd = kept.Y + ((int64_t)blockIdx.x * w.NC + c) * C * kept.dvp + col;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) yd[(int64_t)(16 * mt + 4 * gr + r) * kept.dvp] = Y[mt][r];
+        const float end = co[C - 1];
+#pragma unroll
+        for (int t = 0; t < 2 * DS; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[t][r] *= end;
+#pragma unroll
+        for (int gp = 0; gp < GP; ++gp) {
+            float x[8], y[8];
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+                const f32x4 ev = *reinterpret_cast<const f32x4 *>(co + 32 * gp + 16 * hf + 4 * gr);
+                const f32x4 be = *reinterpret_cast<const f32x4 *>(co + C + 32 * gp + 16 * hf + 4 * gr);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    x[4 * hf + r] = a.scale * ev[r] * o[2 * gp + hf][r];
+                    y[4 * hf + r] = -be[r] * ev[r] * Y[2 * gp + hf][r];
+                }
+            }
+            const Terms<3> xt = split<3>(x), yt = split<3>(y);
+#pragma unroll
+            for (int t = 0; t < 2 * DS; ++t) {
+                mma<NT, 3>(S[t], frag<NT>(QT + (t * GP + gp) * NT * FRAG, lane), xt);
+                mma<NT, 3>(S[t], frag<NT>(KT + (t * GP + gp) * NT * FRAG, lane), yt);
+            }
+        }
+    }
+    if (!live || !d_first) return;
+#pragma unroll
+    for (int t = 0; t < 2 * DS; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int d = 16 * t + 4 * gr + r;
+            if (d < a.dk) d_first[s0 + (int64_t)d * a.dv] = S[t][r];
+        }
+}
+
+constexpr int GRAD_WAVES = 8, GRAD_THREADS = GRAD_WAVES * 64;
+
+template <class E, int DS>
+struct GradLds {
+    using B = Lay<E, DS>;
+    static constexpr int PITCH = B::C + 4, SQ = B::C * PITCH * 4;
+    static constexpr int ONE = B::MT * (B::NT + 6) * FRAG;  // dO, Y, U of 32 columns
+    static constexpr int TRI = B::TRI * 3 * FRAG;           // N, M, N^T, (beta M)^T: four of these
+    static constexpr int SUMS = (2 * GRAD_WAVES + 2) * B::C * 4 + GRAD_WAVES * 4;
+    // the staged columns and M, N as floats are done with before the four triangles are read
+    static constexpr int AT_SQ = ONE, AT_TRI = ONE + 2 * SQ, AT_SUMS = AT_TRI + 4 * TRI;
+    static constexpr int AT_GAM = AT_SUMS + (SUMS + 15) / 16 * 16, BYTES = AT_GAM + B::C * 8 + 4 * B::C * 4;
+};
+
+// Grid (chunk, b * Hk + key head): everything of the list above that has no
+// order.  A wave owns 16 of the dk columns of dq, r and c (every eighth tile);
+// the sums over dv go by groups of 32 columns whose fragments all waves share,
+// and the tiles of M and N are dealt out among the waves.  The value heads of a
+// key head follow each other, so that their dq and dk add up in registers.
+template <class E, int DS>
+__global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
+    const E *__restrict__ q, const E *__restrict__ k, const E *__restrict__ v, const float *__restrict__ g,
+    const E *__restrict__ d_out, Args a, const int32_t *__restrict__ lengths, Chunks w, Kept kept, E *__restrict__ d_q,
+    E *__restrict__ d_k, E *__restrict__ d_v, float *__restrict__ d_g, float *__restrict__ d_beta) {
+    using F = Blob<E, DS, true>;
+    using G = GradLds<E, DS>;
+    constexpr int C = F::C, MT = F::MT, NT = F::NT, GP = F::GP, PITCH = G::PITCH;
+    constexpr int TW = (2 * DS + GRAD_WAVES - 1) / GRAD_WAVES;  // dk tiles of a wave
+    constexpr int LT = MT * (MT + 1) / 2, LW = (2 * LT + GRAD_WAVES - 1) / GRAD_WAVES;  // tiles of M and N
+    extern __shared__ char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, gr = lane >> 4;
+    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int chunk = blockIdx.x, b = blockIdx.y / a.Hk, hk = blockIdx.y % a.Hk, rep = a.Hv / a.Hk;
+    const int n = (lengths ? max(0, min(a.L, lengths[b])) : a.L) - chunk * C;
+    if (n <= 0) return;
+    char *fo = lds, *fy = fo + MT * NT * FRAG, *fu = fy + MT * 3 * FRAG;
+    float *sqM = reinterpret_cast<float *>(lds + G::AT_SQ), *sqN = sqM + C * PITCH;
+    char *tri = lds + G::AT_TRI;  // N, M, N^T, (beta M)^T
+    float *sums = reinterpret_cast<float *>(lds + G::AT_SUMS);  // [waves][2][C], then y.v, beta; then the ends
+    float *yv = sums + 2 * GRAD_WAVES * C, *ends = yv + 2 * C;
+    double *gam = reinterpret_cast<double *>(lds + G::AT_GAM);
+    float *co = reinterpret_cast<float *>(gam + C);  // E, beta, last
+    const char *key = w.key + ((int64_t)blockIdx.y * w.NC + chunk) * F::KEY;
+    const int64_t row0 = (int64_t)b * a.L + chunk * C;
+
+    f32x4 dqs[TW][MT], dks[TW][MT];
+#pragma unroll
+    for (int p = 0; p < TW; ++p)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) dqs[p][mt] = dks[p][mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+
+    for (int hr = 0; hr < rep; ++hr) {
+        const int h = hk * rep + hr;
+        const int64_t bh = (int64_t)b * a.Hv + h, ch = bh * w.NC + chunk;
+        const float *cog = reinterpret_cast<const float *>(w.head + ch * F::HEAD + F::T);
+        if (tid < 64) {
+            double s = tid < C && tid < n ? log_decay(g[(row0 + tid) * a.Hv + h]) : 0.0;
+#pragma unroll
+            for (int o = 1; o < C; o <<= 1) {
+                const double p = __shfl_up(s, o, 64);
+                if (tid >= o) s += p;
+            }
+            if (tid < C) gam[tid] = s;
+        }
+        for (int i = tid; i < 3 * C; i += GRAD_THREADS) co[i] = cog[i];
+        const float *S = kept.S + ch * 32 * DS * kept.dvp, *dS = kept.dS + ch * 32 * DS * kept.dvp;
+        const float *U = kept.U + ch * C * kept.dvp, *Y = kept.Y + ch * C * kept.dvp;
+        f32x4 dq[TW][MT], rr[TW][MT], cc[TW][MT], mn[LW];
+#pragma unroll
+        for (int p = 0; p < TW; ++p)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) dq[p][mt] = rr[p][mt] = cc[p][mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int l = 0; l < LW; ++l) mn[l] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        float dot = 0.0f;   // <dS, S>, the lane's part
+        float yvp = 0.0f;   // y.v of row 16 wv + m, the lane's part (waves below MT)
+        for (int vg = 0; vg < kept.dvp / 32; ++vg) {
+            __syncthreads();  // the staged columns (and, at first, the coefficients) may be written
+            for (int task = wv; task < 3 * MT; task += GRAD_WAVES) {
+                const int which = task / MT, mt = task % MT, i = 16 * mt + m;  // Y, U, dO (Y of tile mt: wave mt)
+                float x[8];
+                if (which < 2) {
+                    const float *p = (which ? U : Y) + (int64_t)i * kept.dvp + 32 * vg + 4 * gr;
+                    const f32x4 x0 = *reinterpret_cast<const f32x4 *>(p), x1 = *reinterpret_cast<const f32x4 *>(p + 16);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[r] = x0[r], x[4 + r] = x1[r];
+                    put_frag<3>((which ? fu : fy) + mt * 3 * FRAG, lane, split<3>(x));
+                    if (which == 0 && i < n) {
+                        const int64_t vrow = ((row0 + i) * a.Hv + h) * a.dv;
+                        const float be = co[C + i];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const int cv = 32 * vg + slot(gr, j);
+                            if (cv < a.dv) {
+                                yvp += x[j] * to_float(v[vrow + cv]);
+                                d_v[vrow + cv] = from_float<E>(be * x[j]);
+                            }
+                        }
+                    }
+                } else {
+                    const int64_t vrow = ((row0 + i) * a.Hv + h) * a.dv;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int cv = 32 * vg + slot(gr, j);
+                        x[j] = i < n && cv < a.dv ? to_float(d_out[vrow + cv]) : 0.0f;
+                    }
+                    put_frag<NT>(fo + mt * NT * FRAG, lane, split<NT>(x));
+                }
+            }
+            __syncthreads();
+#pragma unroll
+            for (int p = 0; p < TW; ++p) {
+                const int t = p * GRAD_WAVES + wv;
+                if (t >= 2 * DS) continue;
+                const float *ps = S + (int64_t)(16 * t + m) * kept.dvp + 32 * vg + 4 * gr;
+                const float *pd = dS + (int64_t)(16 * t + m) * kept.dvp + 32 * vg + 4 * gr;
+                const f32x4 s0 = *reinterpret_cast<const f32x4 *>(ps), s1 = *reinterpret_cast<const f32x4 *>(ps + 16);
+                const f32x4 e0 = *reinterpret_cast<const f32x4 *>(pd), e1 = *reinterpret_cast<const f32x4 *>(pd + 16);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) dot += s0[r] * e0[r] + s1[r] * e1[r];
+                const Terms<3> st = split<3>(s0, s1), et = split<3>(e0, e1);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    mma<NT, 3>(dq[p][mt], frag<NT>(fo + mt * NT * FRAG, lane), st);
+                    mma<3, 3>(rr[p][mt], frag<3>(fy + mt * 3 * FRAG, lane), st);
+                    mma<3, 3>(cc[p][mt], frag<3>(fu + mt * 3 * FRAG, lane), et);
+                }
+            }
+#pragma unroll
+            for (int l = 0; l < LW; ++l) {
+                const int idx = l * GRAD_WAVES + wv;
+                if (idx >= 2 * LT) continue;
+                int mt = 0, nt = idx % LT;
+                while (nt > mt) nt -= ++mt;
+                if (idx < LT) mma<3, 3>(mn[l], frag<3>(fy + mt * 3 * FRAG, lane), frag<3>(fu + nt * 3 * FRAG, lane));
+                else mma<NT, 3>(mn[l], frag<NT>(fo + mt * NT * FRAG, lane), frag<3>(fu + nt * 3 * FRAG, lane));
+            }
+        }
+#pragma unroll
+        for (int l = 0; l < LW; ++l) {
+            const int idx = l * GRAD_WAVES + wv;
+            if (idx >= 2 * LT) continue;
+            int mt = 0, nt = idx % LT;
+            while (nt > mt) nt -= ++mt;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 16 * mt + 4 * gr + r, j = 16 * nt + m;
+                const float d = j <= i ? expf((float)(gam[i] - gam[j])) : 0.0f;
+                if (idx < LT) sqM[i * PITCH + j] = j < i ? d * mn[l][r] : 0.0f;
+                else sqN[i * PITCH + j] = a.scale * d * mn[l][r];
+            }
+        }
+        if (wv < MT) {
+            yvp += __shfl_xor(yvp, 16, 64);
+            yvp += __shfl_xor(yvp, 32, 64);
+            if (gr == 0) yv[16 * wv + m] = yvp;
+        }
+#pragma unroll
+        for (int s = 32; s >= 1; s >>= 1) dot += __shfl_xor(dot, s, 64);
+        if (lane == 0) ends[wv] = co[C - 1] * dot;
+        __syncthreads();
+        for (int u = tid; u < 4 * F::TRI * 64; u += GRAD_THREADS) {
+            const int f4 = u >> 6, which = f4 / F::TRI, f = f4 % F::TRI;  // N, M, N^T, (beta M)^T
+            int mt, gp;
+            if (which < 2) tri_at<MT, false>(f, &mt, &gp);
+            else tri_at<MT, true>(f, &mt, &gp);
+            const int i = 16 * mt + m;
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int c = 32 * gp + slot(gr, j), lo = which < 2 ? c : i, hi = which < 2 ? i : c;
+                x[j] = lo <= hi ? (which & 1 ? sqM : sqN)[hi * PITCH + lo] : 0.0f;
+                if (which == 3) x[j] *= co[C + hi];
+            }
+            put_frag<3>(tri + which * G::TRI + f * 3 * FRAG, lane, split<3>(x));
+        }
+        __syncthreads();
+        float pg[MT][4], pb[MT][4], pe = 0.0f;  // row sums: dgamma, k.r; k.(last U dS^T) of all rows
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) pg[mt][r] = pb[mt][r] = 0.0f;
+#pragma unroll
+        for (int p = 0; p < TW; ++p) {
+            const int t = p * GRAD_WAVES + wv, d = 16 * t + m;
+            if (t >= 2 * DS) continue;
+            Terms<NT> kt[GP], qt[GP];
+#pragma unroll
+            for (int gp = 0; gp < GP; ++gp) {
+                kt[gp] = frag<NT>(key + F::K + (t * GP + gp) * NT * FRAG, lane);
+                qt[gp] = frag<NT>(key + F::K + F::KT + (t * GP + gp) * NT * FRAG, lane);
+            }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                const f32x4 ev = *reinterpret_cast<const f32x4 *>(co + 16 * mt + 4 * gr);
+                const f32x4 be = *reinterpret_cast<const f32x4 *>(co + C + 16 * mt + 4 * gr);
+                const f32x4 la = *reinterpret_cast<const f32x4 *>(co + 2 * C + 16 * mt + 4 * gr);
+                f32x4 x = a.scale * ev * dq[p][mt], y = (f32x4){0.f, 0.f, 0.f, 0.f} - ev * rr[p][mt], z = la * cc[p][mt];
+                float kk[4], qq[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = 16 * mt + 4 * gr + r;
+                    const int64_t at = ((row0 + i) * a.Hk + hk) * a.dk + d;
+                    const bool in = i < n && d < a.dk;
+                    kk[r] = in ? to_float(k[at]) : 0.0f;
+                    qq[r] = in ? to_float(q[at]) : 0.0f;
+                    pe += kk[r] * z[r];
+                }
+                f32x4 mk = {0.f, 0.f, 0.f, 0.f}, mc = mk;
+#pragma unroll
+                for (int gp = 0; gp < GP; ++gp) {
+                    if (gp <= mt / 2) {
+                        mma<3, NT>(x, frag<3>(tri + F::lower(mt, gp) * 3 * FRAG, lane), kt[gp]);
+                        mma<3, NT>(mk, frag<3>(tri + G::TRI + F::lower(mt, gp) * 3 * FRAG, lane), kt[gp]);
+                    }
+                    if (gp >= mt / 2) {
+                        mma<3, NT>(z, frag<3>(tri + 2 * G::TRI + F::upper(mt, gp) * 3 * FRAG, lane), qt[gp]);
+                        mma<3, NT>(mc, frag<3>(tri + 3 * G::TRI + F::upper(mt, gp) * 3 * FRAG, lane), kt[gp]);
+                    }
+                }
+                y -= mk;
+                z -= mc;
+                dqs[p][mt] += x;
+                dks[p][mt] += be * y + z;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    pb[mt][r] += kk[r] * y[r];
+                    pg[mt][r] += qq[r] * x[r] + be[r] * (kk[r] * y[r]) - kk[r] * z[r];
+                }
+            }
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+#pragma unroll
+                for (int s = 8; s >= 1; s >>= 1) {
+                    pg[mt][r] += __shfl_xor(pg[mt][r], s, 64);
+                    pb[mt][r] += __shfl_xor(pb[mt][r], s, 64);
+                }
+                if (m == 0) {
+                    sums[(2 * wv) * C + 16 * mt + 4 * gr + r] = pg[mt][r];
+                    sums[(2 * wv + 1) * C + 16 * mt + 4 * gr + r] = pb[mt][r];
+                }
+            }
+#pragma unroll
+        for (int s = 32; s >= 1; s >>= 1) pe += __shfl_xor(pe, s, 64);
+        if (lane == 0) ends[wv] += pe;
+        __syncthreads();
+        if (tid < 64) {
+            double x = 0.0;
+            float y = tid < C ? yv[tid] : 0.0f;
+            for (int q8 = 0; q8 < GRAD_WAVES; ++q8) {
+                if (tid < C) {
+                    x += sums[2 * q8 * C + tid];
+                    y += sums[(2 * q8 + 1) * C + tid];
+                }
+                if (tid == C - 1) x += ends[q8];
+            }
+#pragma unroll
+            for (int o = 1; o < C; o <<= 1) {  // the sum from tid on
+                const double p = __shfl_down(x, o, 64);
+                if (tid + o < C) x += p;
+            }
+            if (tid < C && tid < n) {
+                d_g[(row0 + tid) * a.Hv + h] = (float)x;
+                d_beta[(row0 + tid) * a.Hv + h] = y;
+            }
+        }
+        __syncthreads();  // gam, co and the sums are written again
+    }
+#pragma unroll
+    for (int p = 0; p < TW; ++p) {
+        const int t = p * GRAD_WAVES + wv, d = 16 * t + m;
+        if (t >= 2 * DS || d >= a.dk) continue;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 16 * mt + 4 * gr + r;
+                if (i >= n) continue;
+                const int64_t at = ((row0 + i) * a.Hk + hk) * a.dk + d;
+                d_q[at] = from_float<E>(dqs[p][mt][r]);
+                d_k[at] = from_float<E>(dks[p][mt][r]);
+            }
+    }
+}
+
+namespace {
+
+template <class E, int DS>
+size_t carve(void *ws, const Args &a, Chunks *w, Kept *kept) {
+    using F = Blob<E, DS, true>;
+    spk::Carver c(ws);
+    const size_t bh = (size_t)a.B * a.Hv;
+    w->NC = (a.L + F::C - 1) / F::C;
+    kept->dvp = (a.dv + 31) / 32 * 32;
+    w->key = c.take<char>((size_t)a.B * a.Hk * w->NC * F::KEY);
+    w->head = c.take<char>(bh * w->NC * F::HEAD);
+    kept->S = c.take<float>(bh * w->NC * 32 * DS * kept->dvp);
+    kept->dS = c.take<float>(bh * w->NC * 32 * DS * kept->dvp);
+    kept->U = c.take<float>(bh * w->NC * F::C * kept->dvp);
+    kept->Y = c.take<float>(bh * w->NC * F::C * kept->dvp);
+    return spk::align_up(c.off, 256);
+}
+
+struct Call {
+    const void *q, *k, *v;
+    const float *g, *beta;
+    const int32_t *lengths;
+    const float *state_in;
+    const void *d_out;
+    const float *d_last;
+    void *d_q, *d_k, *d_v;
+    float *d_g, *d_beta, *d_first;
+};
+
+template <class E, int DS>
+int backward(const Call &c, const Args &a, void *ws, hipStream_t st, const char *name) {
+    using F = Blob<E, DS, true>;
+    constexpr int LP = PrepLds<E, DS>::BYTES, LG = GradLds<E, DS>::BYTES;
+    Chunks w;
+    Kept kept;
+    carve<E, DS>(ws, a, &w, &kept);
+    const E *q = static_cast<const E *>(c.q), *k = static_cast<const E *>(c.k), *v = static_cast<const E *>(c.v);
+    const E *d_out = static_cast<const E *>(c.d_out);
+    const dim3 per_key((unsigned)w.NC, (unsigned)(a.B * a.Hk));
+    hipLaunchKernelGGL((k_delta_prep<E, DS, true>), per_key, dim3(PREP_THREADS), LP, st, q, k, c.g, c.beta, a, c.lengths, wide_rows<E>(a.dk, q, k), w);
+    const int tiles = kept.dvp / 16, compute = scan_waves(a, tiles);
+    const dim3 cols((unsigned)(a.B * a.Hv), (unsigned)((tiles + compute - 1) / compute));
+    const dim3 threads(64 * std::max(4, compute));
+    constexpr int NB = 2 * F::SCAN <= LDS_BYTES ? 2 : 1;
+    hipLaunchKernelGGL((k_delta_scan<E, DS, NB, true>), cols, threads, NB * F::SCAN, st, v, a, c.lengths, compute, w,
+                       c.state_in, (E *)nullptr, (float *)nullptr, kept);
+    constexpr int ONE = F::KEY + F::HEAD - F::T, NR = 2 * ONE <= LDS_BYTES ? 2 : 1;
+    static_assert(ONE <= LDS_BYTES && F::SCAN <= LDS_BYTES && LP <= LDS_BYTES && LG <= LDS_BYTES, "LDS");
+    hipLaunchKernelGGL((k_delta_rscan<E, DS, NR>), cols, threads, NR * ONE, st, d_out, a, c.lengths, compute, w, kept,
+                       c.d_last, c.d_first);
+    hipLaunchKernelGGL((k_delta_grads<E, DS>), per_key, dim3(GRAD_THREADS), LG, st, q, k, v, c.g, d_out, a, c.lengths, w, kept, static_cast<E *>(c.d_q), static_cast<E *>(c.d_k),
+                       static_cast<E *>(c.d_v), c.d_g, c.d_beta);
+    return spk::check_launch(name);
+}
+
+size_t workspace_bytes(const Args &a) {
+    Chunks w;
+    Kept kept;
+#define SPK_WS(DS) \
+    return a.dtype == SPK_F32 ? carve<float, DS>(nullptr, a, &w, &kept) : carve<uint16_t, DS>(nullptr, a, &w, &kept)
+    SPK_DELTA_FORMS(SPK_WS)
+#undef SPK_WS
+}
+
+int run(const Call &c, const Args &a, void *ws, hipStream_t st, const char *name) {
+#define SPK_BW(DS) \
+    return a.dtype == SPK_F32 ? backward<float, DS>(c, a, ws, st, name) : backward<uint16_t, DS>(c, a, ws, st, name)
+    SPK_DELTA_FORMS(SPK_BW)
+#undef SPK_BW
+}
+
+// No samples: the gradient passes through.
+__global__ __launch_bounds__(256) void k_pass(const float *src, float *dst, int64_t n) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256)
+        dst[i] = src ? src[i] : 0.0f;
+}
+
+}  // namespace
+}  // namespace delta
+}  // namespace spk
+
+using namespace spk::delta;
+
+extern "C" size_t spk_delta_rule_backward_workspace_size(int dtype, int B, int L, int Hk, int Hv, int dk, int dv) {
+    const Args a{dtype, B, L, Hk, Hv, dk, dv, 1.0f};
+    return check(a, "") == SPK_OK && B > 0 && L > 0 ? workspace_bytes(a) : 0;
+}
+
+extern "C" int spk_delta_rule_backward(const void *q, const void *k, const void *v, const float *g, const float *beta,
+                                       int dtype, int B, int L, int Hk, int Hv, int dk, int dv, float scale,
+                                       const int32_t *lengths, const float *initial_state, const void *d_out,
+                                       const float *d_final_state, void *d_q, void *d_k, void *d_v, float *d_g,
+                                       float *d_beta, float *d_initial_state, void *workspace, size_t ws_bytes,
+                                       void *stream) {
+    const char *name = "spk_delta_rule_backward";
+    const Args a{dtype, B, L, Hk, Hv, dk, dv, scale};
+    if (int rc = check(a, name)) return rc;
+    if (B == 0) return spk::ok();
+    hipStream_t st = spk::as_stream(stream);
+    if (L == 0) {
+        if (!d_initial_state) return spk::ok();
+        const int64_t n = (int64_t)B * Hv * dk * dv;
+        hipLaunchKernelGGL(k_pass, dim3((unsigned)std::min<int64_t>(4096, spk::ceil_div(n, 256))), dim3(256), 0, st,
+                           d_final_state, d_initial_state, n);
+        return spk::check_launch(name);
+    }
+    SPK_REQUIRE(q && k && v && g && beta && d_out && d_q && d_k && d_v && d_g && d_beta, SPK_E_ARG,
+                "%s: all inputs, d_out and the gradients d_q, d_k, d_v, d_g and d_beta are required", name);
+    const size_t need = workspace_bytes(a);
+    SPK_REQUIRE(workspace && ws_bytes >= need, SPK_E_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", name,
+                workspace ? ws_bytes : (size_t)0, need);
+    const Call c{q, k, v, g, beta, lengths, initial_state, d_out, d_final_state, d_q, d_k, d_v, d_g, d_beta,
+                 d_initial_state};
+    return run(c, a, workspace, st, name);
+}

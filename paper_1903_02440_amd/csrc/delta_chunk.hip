@@ -1,382 +1,16 @@
-// The gated delta rule over chunks of samples (gfx950): operands of all chunks
-// at once, then the states from chunk to chunk.  The formulas and the operands'
-// layout are in delta_chunk.hpp.
+// The gated delta rule over chunks of samples (gfx950): the batch call.  The
+// formulas and the operands' layout are in delta_chunk.hpp, the kernels that it
+// shares with the backward pass in delta_kernels.hpp.
 #include <algorithm>
 
-#include "delta_chunk.hpp"
+#include "delta_kernels.hpp"
 
 namespace spk {
 namespace delta {
 
-// Workspace: per (sequence, key head, chunk) K, K^T and Q; per (sequence,
-// value head, chunk) T, P and the coefficients.
-template <class E, int DS>
-struct Fwd : Lay<E, DS> {
-    using B = Lay<E, DS>;
-    static constexpr int KEY = 2 * B::K + B::KT;
-    static constexpr int T = B::TRI * 3 * FRAG, P = B::TRI * B::NP * FRAG;
-    static constexpr int HEAD = T + P + B::COEF;
-};
-
-struct Chunks {
-    int NC;               // chunks of the longest sequence
-    char *key, *head;     // workspace
-};
-
-// Eight elements of a row of keys or queries, 0 past its end.
-template <class E>
-__device__ __forceinline__ void load8(const E *p, int s, int g, int dk, bool wide, float (&x)[8]) {
-    // (elements 0..3 and 4..7 are runs of 4; wide: both are whole and aligned)
-    const int c0 = 32 * s + 4 * g;
-    if (wide) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int c = c0 + 16 * h;
-            if (c < dk) {
-                if constexpr (sizeof(E) == 4) {
-                    const float4 w = *reinterpret_cast<const float4 *>(p + c);
-                    x[4 * h] = w.x, x[4 * h + 1] = w.y, x[4 * h + 2] = w.z, x[4 * h + 3] = w.w;
-                } else {
-                    const uint2 w = *reinterpret_cast<const uint2 *>(p + c);
-                    x[4 * h] = __uint_as_float(w.x << 16), x[4 * h + 1] = __uint_as_float(w.x & 0xFFFF0000u);
-                    x[4 * h + 2] = __uint_as_float(w.y << 16), x[4 * h + 3] = __uint_as_float(w.y & 0xFFFF0000u);
-                }
-            } else {
-                x[4 * h] = x[4 * h + 1] = x[4 * h + 2] = x[4 * h + 3] = 0.0f;
-            }
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int c = 32 * s + slot(g, j);
-            x[j] = c < dk ? to_float(p[c]) : 0.0f;
-        }
-    }
-}
-
-constexpr int PREP_THREADS = 256;
-
-// LDS of the operand kernel: the fragments of K and Q, whose room A and T take
-// once the products are made; then the products K K^T and Q K^T.
-template <class E, int DS>
-struct PrepLds {
-    using B = Lay<E, DS>;
-    static constexpr int PITCH = B::C + 4;  // floats; 16-byte rows, four banks on from row to row
-    static constexpr int SQ = B::C * PITCH * 4;
-    static constexpr int R0 = 2 * B::K > 2 * SQ ? 2 * B::K : 2 * SQ;
-    static constexpr int BYTES = R0 + 2 * SQ + B::C * 8 + B::C * 4;
-};
-
-// Grid (chunk, b * Hk + key head): the fragments of the chunk's keys and
-// queries, their products, and for each value head of the key head T, P and the
-// coefficients.  T by blocks of 16: the diagonal ones by substitution, a column
-// a lane; the rest of block column j by
-//     T_ij = -T_ii sum over j <= m < i of A_im T_mj
-// on the float matrix cores, a block column a wave.
-template <class E, int DS>
-__global__ __launch_bounds__(PREP_THREADS) void k_delta_prep(const E *__restrict__ q, const E *__restrict__ k,
-                                                             const float *__restrict__ g,
-                                                             const float *__restrict__ beta, Args a,
-                                                             const int32_t *__restrict__ lengths, int wide, Chunks w) {
-    using F = Fwd<E, DS>;
-    using S = PrepLds<E, DS>;
-    constexpr int C = F::C, MT = F::MT, NT = F::NT, GP = F::GP, PITCH = S::PITCH;
-    extern __shared__ char lds[];
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, m = lane & 15, gr = lane >> 4;
-    const int chunk = blockIdx.x, b = blockIdx.y / a.Hk, hk = blockIdx.y % a.Hk, rep = a.Hv / a.Hk;
-    const int n = (lengths ? max(0, min(a.L, lengths[b])) : a.L) - chunk * C;  // samples from the chunk's first on
-    if (n <= 0) return;
-    char *fk = lds, *fq = lds + F::K;
-    float *A = reinterpret_cast<float *>(lds), *T = A + C * PITCH;
-    float *G = reinterpret_cast<float *>(lds + S::R0), *H = G + C * PITCH;
-    double *gam = reinterpret_cast<double *>(lds + S::R0 + 2 * S::SQ);
-    float *bet = reinterpret_cast<float *>(gam + C);
-    char *key = w.key + ((int64_t)blockIdx.y * w.NC + chunk) * F::KEY;
-
-    // K and Q
-    for (int u = tid; u < 2 * MT * DS * 64; u += PREP_THREADS) {
-        const int f = u >> 6, mt = f / DS % MT, s = f % DS;  // (lane = u & 63)
-        const bool isq = f >= MT * DS;
-        const int i = 16 * mt + m;
-        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (i < n) load8<E>((isq ? q : k) + (((int64_t)b * a.L + chunk * C + i) * a.Hk + hk) * a.dk, s, gr, a.dk, wide, x);
-        const Terms<NT> t = split<NT>(x);
-        const int o = (mt * DS + s) * NT * FRAG;
-        put_frag<NT>((isq ? fq : fk) + o, lane, t);
-        put_frag<NT>(key + (isq ? F::K + F::KT : 0) + o, lane, t);
-    }
-    __syncthreads();
-    // K^T: row d = 16 t + m, samples slot(gr, j) of group gp
-    for (int u = tid; u < 2 * DS * GP * NT * 64; u += PREP_THREADS) {
-        const int f = u >> 6, term = f % NT, gp = f / NT % GP, t = f / (NT * GP);
-        const int d = 16 * t + m, s = d >> 5, r = d & 31, gd = (r & 15) >> 2, jd = (r >> 4) * 4 + (r & 3);
-        uint16_t e[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int i = 32 * gp + slot(gr, j);
-            e[j] = *reinterpret_cast<const uint16_t *>(fk + (((i >> 4) * DS + s) * NT + term) * FRAG +
-                                                       (gd * 16 + (i & 15)) * 16 + jd * 2);
-        }
-        u32x4 o;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) o[j] = (uint32_t)e[2 * j] | ((uint32_t)e[2 * j + 1] << 16);
-        *reinterpret_cast<u32x4 *>(key + F::K + f * FRAG + lane * 16) = o;
-    }
-    // lower tiles of K K^T (rows 0..MT-1 of the list) and Q K^T (the rest, from the last row on)
-    for (int row = wv; row < 2 * MT; row += PREP_THREADS / 64) {
-        const bool isq = row >= MT;
-        const int mt = isq ? 2 * MT - 1 - row : row;
-        const char *fa = isq ? fq : fk;
-        for (int nt = 0; nt <= mt; ++nt) {
-            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int s = 0; s < DS; ++s)
-                mma<NT, NT>(acc, frag<NT>(fa + (mt * DS + s) * NT * FRAG, lane),
-                            frag<NT>(fk + (nt * DS + s) * NT * FRAG, lane));
-#pragma unroll
-            for (int r = 0; r < 4; ++r) (isq ? H : G)[(16 * mt + 4 * gr + r) * PITCH + 16 * nt + m] = acc[r];
-        }
-    }
-    __syncthreads();  // the fragments' room is free
-    for (int hr = 0; hr < rep; ++hr) {
-        const int h = hk * rep + hr;
-        char *head = w.head + (((int64_t)b * a.Hv + h) * w.NC + chunk) * F::HEAD;
-        if (tid < 64) {
-            const int64_t at = ((int64_t)b * a.L + chunk * C + tid) * a.Hv + h;
-            const bool in = tid < C && tid < n;
-            double s = in ? log_decay(g[at]) : 0.0;
-#pragma unroll
-            for (int o = 1; o < C; o <<= 1) {
-                const double p = __shfl_up(s, o, 64);
-                if (tid >= o) s += p;
-            }
-            const double end = __shfl(s, C - 1, 64);
-            if (tid < C) {
-                const float be = in ? beta[at] : 0.0f;
-                gam[tid] = s;
-                bet[tid] = be;
-                float *co = reinterpret_cast<float *>(head + F::T + F::P);
-                co[tid] = expf((float)s);
-                co[C + tid] = be;
-                co[2 * C + tid] = expf((float)(end - s));
-            }
-        }
-        __syncthreads();
-        for (int e = tid; e < C * C; e += PREP_THREADS) {
-            const int i = e / C, j = e % C;
-            if (j < i) A[i * PITCH + j] = bet[i] * expf((float)(gam[i] - gam[j])) * G[i * PITCH + j];
-        }
-        for (int u = tid; u < F::TRI * 64; u += PREP_THREADS) {  // P
-            const int f = u >> 6;
-            const int mt = MT == 4 && f >= 2 ? 2 + ((f - 2) >> 1) : f, gp = MT == 4 && f >= 2 ? (f - 2) & 1 : 0;
-            const int i = 16 * mt + m;
-            float x[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int c = 32 * gp + slot(gr, j);
-                x[j] = c <= i ? expf((float)(gam[i] - gam[c])) * H[i * PITCH + c] : 0.0f;
-            }
-            put_frag<F::NP>(head + F::T + f * F::NP * FRAG, lane, split<F::NP>(x));
-        }
-        __syncthreads();
-        if (wv < MT) {  // diagonal block wv, column m (all lane groups alike)
-            const float *Ab = A + 16 * wv * PITCH + 16 * wv;
-            float x[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float s = i == m ? 1.0f : 0.0f;
-#pragma unroll
-                for (int j = 0; j < i; ++j) s -= Ab[i * PITCH + j] * x[j];
-                x[i] = s;
-            }
-            if (gr == 0) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) T[(16 * wv + i) * PITCH + 16 * wv + m] = x[i];
-            }
-        }
-        __syncthreads();
-        if (wv < MT - 1) {  // block column wv
-            f32x4 tc[MT];
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                if (i < wv) continue;
-                if (i == wv) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) tc[i][r] = T[(16 * i + 4 * gr + r) * PITCH + 16 * i + m];
-                    continue;
-                }
-                f32x4 s = {0.f, 0.f, 0.f, 0.f}, o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int c = 0; c < MT; ++c) {
-                    if (c < wv || c >= i) continue;
-                    const f32x4 al = *reinterpret_cast<const f32x4 *>(A + (16 * i + m) * PITCH + 16 * c + 4 * gr);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) s = __builtin_amdgcn_mfma_f32_16x16x4f32(al[r], tc[c][r], s, 0, 0, 0);
-                }
-                const f32x4 tl = *reinterpret_cast<const f32x4 *>(T + (16 * i + m) * PITCH + 16 * i + 4 * gr);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) o = __builtin_amdgcn_mfma_f32_16x16x4f32(tl[r], -s[r], o, 0, 0, 0);
-                tc[i] = o;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) T[(16 * i + 4 * gr + r) * PITCH + 16 * wv + m] = o[r];
-            }
-        }
-        __syncthreads();
-        for (int u = tid; u < F::TRI * 64; u += PREP_THREADS) {
-            const int f = u >> 6;
-            const int mt = MT == 4 && f >= 2 ? 2 + ((f - 2) >> 1) : f, gp = MT == 4 && f >= 2 ? (f - 2) & 1 : 0;
-            const int i = 16 * mt + m;
-            float x[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int c = 32 * gp + slot(gr, j);
-                x[j] = c <= i ? T[i * PITCH + c] : 0.0f;
-            }
-            put_frag<3>(head + f * 3 * FRAG, lane, split<3>(x));
-        }
-        __syncthreads();
-    }
-}
-
-// Grid (b * Hv + value head, block of columns): a wave carries 16 columns of the
-// state through the chunks, in registers: as the right operand of K S and Q S
-// (three terms) and as the sums of K^T (last U).  The waves of a workgroup share
-// the chunk's operands in LDS and wait for each other only there.  NBUF buffers:
-// with two, the next chunk's operands are on their way during this one's products.
-template <class E, int DS, int NBUF>
-__global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Args a,
-                                                    const int32_t *__restrict__ lengths, int compute, Chunks w,
-                                                    const float *state_in, E *__restrict__ out, float *state_out) {
-    using F = Fwd<E, DS>;
-    constexpr int C = F::C, MT = F::MT, NT = F::NT, GP = F::GP, NP = F::NP;
-    extern __shared__ char lds[];
-    const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, gr = lane >> 4;
-    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
-    const int b = blockIdx.x / a.Hv, h = blockIdx.x % a.Hv, hk = h / (a.Hv / a.Hk);
-    const int n = lengths ? max(0, min(a.L, lengths[b])) : a.L, nc = (n + C - 1) / C;
-    const int col = ((int)blockIdx.y * compute + wv) * 16 + m;
-    const bool mine = wv < compute && col - m < a.dv, live = mine && col < a.dv;
-    const int64_t s0 = (int64_t)blockIdx.x * a.dk * a.dv + col;
-    const char *key = w.key + ((int64_t)b * a.Hk + hk) * w.NC * F::KEY;
-    const char *head = w.head + (int64_t)blockIdx.x * w.NC * F::HEAD;
-    f32x4 S[2 * DS];
-#pragma unroll
-    for (int t = 0; t < 2 * DS; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int d = 16 * t + 4 * gr + r;
-            S[t][r] = live && d < a.dk && state_in ? state_in[s0 + (int64_t)d * a.dv] : 0.0f;
-        }
-    auto fetch = [&](int c) {
-        char *dst = lds + (c % NBUF) * (F::KEY + F::HEAD);
-        to_lds(dst, key + (int64_t)c * F::KEY, F::KEY, wv, waves, lane);
-        to_lds(dst + F::KEY, head + (int64_t)c * F::HEAD, F::HEAD, wv, waves, lane);
-    };
-    const int64_t vstep = (int64_t)a.Hv * a.dv;
-    const int64_t v0 = ((int64_t)b * a.L * a.Hv + h) * a.dv + col;
-    if (NBUF == 2 && nc) fetch(0);
-    for (int c = 0; c < nc; ++c) {
-        if (NBUF == 1) {
-            if (c) __syncthreads();
-            fetch(c);
-        }
-        float vv[MT][4];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = c * C + 16 * mt + 4 * gr + r;
-                vv[mt][r] = live && i < n ? to_float(v[v0 + i * vstep]) : 0.0f;
-            }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (NBUF == 2 && c + 1 < nc) fetch(c + 1);
-        if (!mine) continue;
-        const char *K = lds + (c % NBUF) * (F::KEY + F::HEAD), *KT = K + F::K, *Q = KT + F::KT, *T = Q + F::K,
-                   *P = T + F::T;
-        const float *co = reinterpret_cast<const float *>(P + F::P);
-        f32x4 X[MT], Y[MT];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) X[mt] = Y[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s = 0; s < DS; ++s) {
-            const Terms<3> st = split<3>(S[2 * s], S[2 * s + 1]);
-            Terms<NP> sp;
-#pragma unroll
-            for (int i = 0; i < NP; ++i) sp.t[i] = st.t[i];
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                mma<NT, 3>(X[mt], frag<NT>(K + (mt * DS + s) * NT * FRAG, lane), st);
-                mma<NT, NP>(Y[mt], frag<NT>(Q + (mt * DS + s) * NT * FRAG, lane), sp);
-            }
-        }
-        f32x4 U[MT];
-        float e[MT][4];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            const f32x4 ev = *reinterpret_cast<const f32x4 *>(co + 16 * mt + 4 * gr);
-            const f32x4 be = *reinterpret_cast<const f32x4 *>(co + C + 16 * mt + 4 * gr);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                e[mt][r] = ev[r];
-                X[mt][r] = be[r] * (vv[mt][r] - ev[r] * X[mt][r]);
-            }
-            U[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
-        }
-#pragma unroll
-        for (int gp = 0; gp < GP; ++gp) {
-            const Terms<3> rt = split<3>(X[2 * gp], X[2 * gp + 1]);
-#pragma unroll
-            for (int mt = 2 * gp; mt < MT; ++mt) mma<3, 3>(U[mt], frag<3>(T + F::lower(mt, gp) * 3 * FRAG, lane), rt);
-        }
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) Y[mt][r] *= e[mt][r];
-        const float end = co[C - 1];  // E of the last sample
-#pragma unroll
-        for (int t = 0; t < 2 * DS; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) S[t][r] *= end;
-#pragma unroll
-        for (int gp = 0; gp < GP; ++gp) {
-            const Terms<NP> ut = split<NP>(U[2 * gp], U[2 * gp + 1]);
-#pragma unroll
-            for (int mt = 2 * gp; mt < MT; ++mt)
-                mma<NP, NP>(Y[mt], frag<NP>(P + F::lower(mt, gp) * NP * FRAG, lane), ut);
-            const f32x4 l0 = *reinterpret_cast<const f32x4 *>(co + 2 * C + 32 * gp + 4 * gr);
-            const f32x4 l1 = *reinterpret_cast<const f32x4 *>(co + 2 * C + 32 * gp + 16 + 4 * gr);
-            const Terms<3> lt = split<3>(U[2 * gp] * l0, U[2 * gp + 1] * l1);
-#pragma unroll
-            for (int t = 0; t < 2 * DS; ++t)
-                mma<NT, 3>(S[t], frag<NT>(KT + (t * GP + gp) * NT * FRAG, lane), lt);
-        }
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = c * C + 16 * mt + 4 * gr + r;
-                if (live && i < n) out[v0 + i * vstep] = from_float<E>(a.scale * Y[mt][r]);
-            }
-    }
-    if (!live || !state_out) return;
-#pragma unroll
-    for (int t = 0; t < 2 * DS; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int d = 16 * t + 4 * gr + r;
-            if (d < a.dk) state_out[s0 + (int64_t)d * a.dv] = S[t][r];
-        }
-}
-
-int groups_of(int dk) {
-    const int d = (dk + 31) / 32;
-    return d <= 1 ? 1 : d <= 2 ? 2 : d <= 4 ? 4 : 8;
-}
-
 template <class E, int DS>
 size_t carve(void *ws, const Args &a, Chunks *w) {
-    using F = Fwd<E, DS>;
+    using F = Blob<E, DS, false>;
     spk::Carver c(ws);
     w->NC = (a.L + F::C - 1) / F::C;
     w->key = c.take<char>((size_t)a.B * a.Hk * w->NC * F::KEY);
@@ -388,32 +22,23 @@ template <class E, int DS>
 int forward(const void *q, const void *k, const void *v, const float *g, const float *beta, const Args &a,
             const int32_t *lengths, const float *state_in, void *out, float *state_out, void *ws, hipStream_t st,
             const char *name) {
-    using F = Fwd<E, DS>;
+    using F = Blob<E, DS, false>;
     Chunks w;
     carve<E, DS>(ws, a, &w);
     const E *qe = static_cast<const E *>(q), *ke = static_cast<const E *>(k), *ve = static_cast<const E *>(v);
-    const int wide = a.dk % (4) == 0 && ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k)) & (4 * sizeof(E) - 1)) == 0;
+    const int wide = wide_rows<E>(a.dk, q, k);
     constexpr int LP = PrepLds<E, DS>::BYTES;
-    hipLaunchKernelGGL((k_delta_prep<E, DS>), dim3((unsigned)w.NC, (unsigned)(a.B * a.Hk)), dim3(PREP_THREADS), LP, st,
+    hipLaunchKernelGGL((k_delta_prep<E, DS, false>), dim3((unsigned)w.NC, (unsigned)(a.B * a.Hk)), dim3(PREP_THREADS), LP, st,
                        qe, ke, g, beta, a, lengths, wide, w);
-    constexpr int ONE = F::KEY + F::HEAD, NBUF = 2 * ONE <= 160 * 1024 ? 2 : 1;
-    const int tiles = (a.dv + 15) / 16;
-    int compute = std::min(8, tiles);
-    while (compute > 1 && (int64_t)a.B * a.Hv * ((tiles + compute - 1) / compute) < 256) compute = (compute + 1) / 2;
-    const int waves = std::max(4, compute);
-    hipLaunchKernelGGL((k_delta_scan<E, DS, NBUF>),
+    constexpr int ONE = F::SCAN, NBUF = 2 * ONE <= LDS_BYTES ? 2 : 1;
+    static_assert(ONE <= LDS_BYTES && LP <= LDS_BYTES, "LDS");
+    const int tiles = (a.dv + 15) / 16, compute = scan_waves(a, tiles), waves = std::max(4, compute);
+    hipLaunchKernelGGL((k_delta_scan<E, DS, NBUF, false>),
                        dim3((unsigned)(a.B * a.Hv), (unsigned)((tiles + compute - 1) / compute)), dim3(64 * waves),
-                       NBUF * ONE, st, ve, a, lengths, compute, w, state_in, static_cast<E *>(out), state_out);
+                       NBUF * ONE, st, ve, a, lengths, compute, w, state_in, static_cast<E *>(out), state_out,
+                       Kept{});
     return spk::check_launch(name);
 }
-
-#define SPK_DELTA_FORMS(CALL)                     \
-    switch (groups_of(a.dk)) {                    \
-        case 1: CALL(1);                          \
-        case 2: CALL(2);                          \
-        case 4: CALL(4);                          \
-        default: CALL(8);                         \
-    }
 
 size_t chunk_workspace(const Args &a) {
     Chunks w;

@@ -136,6 +136,10 @@ struct Lay {
     static constexpr int COEF = FRAG;              // E, beta, last: f32 [3][C]
     // fragment (mt, gp <= mt / 2) of a lower triangular operand
     static __host__ __device__ constexpr int lower(int mt, int gp) { return mt < 2 ? mt : 2 * mt - 2 + gp; }
+    // fragment (mt, gp >= mt / 2) of an upper triangular one
+    static __host__ __device__ constexpr int upper(int mt, int gp) {
+        return MT == 2 ? mt : mt < 2 ? 2 * mt + gp : mt + 2;
+    }
 };
 
 constexpr int chunk_of(int dtype) { return dtype == SPK_F32 ? 32 : 64; }

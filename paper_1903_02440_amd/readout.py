@@ -1,5 +1,6 @@
 """Binding of the readout operators (``include/libspyke_readout.h``): the gated
-delta rule, its single-sample form, and winners drawn from scores.
+delta rule, its single-sample form and its gradients, and winners drawn from
+scores.
 
 The functions have the names of the C entry points and, as those of the package,
 only marshal: dtype and shape checks, outputs and workspaces that are not given,
@@ -16,6 +17,8 @@ _SIGS = {
     "spk_delta_rule_workspace_size": (_Z, [_I] * 7),
     "spk_delta_rule": (_I, [_P] * 5 + [_I] * 7 + [_F] + [_P] * 5 + [_Z, _P]),
     "spk_delta_rule_step": (_I, [_P] * 5 + [_I] * 6 + [_F] + [_P] * 3),
+    "spk_delta_rule_backward_workspace_size": (_Z, [_I] * 7),
+    "spk_delta_rule_backward": (_I, [_P] * 5 + [_I] * 7 + [_F] + [_P] * 11 + [_Z, _P]),
     "spk_sample_winners_workspace_size": (_Z, [_I] * 5),
     "spk_sample_winners": (_I, [_P, _I, _P, _P] + [_I] * 5 + [_F, _I, _F, _F] + [_P] * 3 + [_Z, _P]),
 }
@@ -51,6 +54,10 @@ def _on(dev, stream, call):
 # ---------------------------------------------------------------- delta rule
 def spk_delta_rule_workspace_size(dtype, B, L, Hk, Hv, dk, dv) -> int:
     return int(_lib.spk_delta_rule_workspace_size(dtype, B, L, Hk, Hv, dk, dv))
+
+
+def spk_delta_rule_backward_workspace_size(dtype, B, L, Hk, Hv, dk, dv) -> int:
+    return int(_lib.spk_delta_rule_backward_workspace_size(dtype, B, L, Hk, Hv, dk, dv))
 
 
 def _delta_args(q, k, v, g, beta, lengths, initial_state):
@@ -121,6 +128,35 @@ def spk_delta_rule_step(q, k, v, g, beta, state, scale=1.0, out=None, stream=Non
         _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), dt, B, Hk, Hv, dk, dv, float(scale), _ptr(state), _ptr(out),
         st))
     return out
+
+
+def spk_delta_rule_backward(q, k, v, g, beta, d_out, d_final_state=None, scale=1.0, initial_state=None, lengths=None,
+                            d_q=None, d_k=None, d_v=None, d_g=None, d_beta=None, d_initial_state=None, workspace=None,
+                            stream=None):
+    """Gradients of spk_delta_rule's (out, final_state) -> (d_q, d_k, d_v, d_g, d_beta, d_initial_state or None)
+    from d_out [B,L,Hv,dv] and d_final_state f32 [B,Hv,dk,dv] (None: zeros).  Rows behind a sequence's length as in
+    spk_delta_rule.  d_initial_state may be d_final_state."""
+    dt, B, L, Hk, Hv, dk, dv = _delta_args(q, k, v, g, beta, lengths, initial_state)
+    dev, f32, state = q.device, torch.float32, (B, Hv, dk, dv)
+    _need(d_out, q.dtype, (B, L, Hv, dv), "d_out")
+    if d_final_state is not None:
+        _need(d_final_state, f32, state, "d_final_state")
+    d_q = _rows(d_q, q, q.dtype, lengths, "d_q")
+    d_k = _rows(d_k, q, q.dtype, lengths, "d_k")
+    d_v = _rows(d_v, v, q.dtype, lengths, "d_v")
+    d_g = _rows(d_g, g, f32, lengths, "d_g")
+    d_beta = _rows(d_beta, g, f32, lengths, "d_beta")
+    d_initial_state = _out(d_initial_state, state, f32, dev, "d_initial_state")
+    n = spk_delta_rule_backward_workspace_size(dt, B, L, Hk, Hv, dk, dv)
+    ws = _ws(workspace, n, dev)
+    _same_device(dev, k=k, v=v, g=g, beta=beta, lengths=lengths, initial_state=initial_state, d_out=d_out,
+                 d_final_state=d_final_state, d_q=d_q, d_k=d_k, d_v=d_v, d_g=d_g, d_beta=d_beta,
+                 d_initial_state=d_initial_state, workspace=ws)
+    _on(dev, stream, lambda st: _lib.spk_delta_rule_backward(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), dt, B, L, Hk, Hv, dk, dv, float(scale), _ptr(lengths),
+        _ptr(initial_state), _ptr(d_out), _ptr(d_final_state), _ptr(d_q), _ptr(d_k), _ptr(d_v), _ptr(d_g),
+        _ptr(d_beta), _ptr(d_initial_state), _ptr(ws), n, st))
+    return d_q, d_k, d_v, d_g, d_beta, (d_initial_state if d_initial_state is not False else None)
 
 
 # ---------------------------------------------------------------- drawing

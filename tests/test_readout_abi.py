@@ -115,3 +115,37 @@ def test_reference_of_a_draw():
     assert ref.sample_winners(x, [0.99], top_k=3)[0][0, 0, 0] == 2  # the later of two equal scores goes
     assert ref.sample_winners(x, [0.0], top_p=0.7)[0][0, 0, 0] == 1
     assert ref.sample_winners(x, [0.99], min_p=0.3)[0][0, 0, 0] == 2
+
+
+def _back(dtype=0, B=2, L=5, Hk=2, Hv=4, dk=8, dv=6, scale=1.0, q=P, dq=P, ws=P, n=1 << 40):
+    return spk.lib().spk_delta_rule_backward(q, P, P, P, P, dtype, B, L, Hk, Hv, dk, dv, scale, None, None, P, None, dq,
+                                             P, P, P, P, None, ws, n, None)
+
+
+def test_backward_refusals():
+    assert _back(dtype=2) == spk.SPK_E_ARG
+    assert _back(dk=0) == spk.SPK_E_SHAPE
+    assert _back(Hv=3) == spk.SPK_E_SHAPE
+    assert _back(L=-1) == spk.SPK_E_SHAPE
+    assert _back(dk=257) == spk.SPK_E_RANGE
+    assert _back(dv=4097) == spk.SPK_E_RANGE
+    assert _back(B=16385) == spk.SPK_E_RANGE
+    assert _back(scale=math.nan) == spk.SPK_E_ARG
+    assert _back(q=None) == spk.SPK_E_ARG
+    assert _back(dq=None) == spk.SPK_E_ARG
+    assert _back(ws=None) == spk.SPK_E_WORKSPACE
+    assert _back(n=1024) == spk.SPK_E_WORKSPACE and b"needed" in spk.lib().spk_last_error()
+    assert _back(B=0) == spk.SPK_OK
+    assert _rule(L=500, ws=None) == spk.SPK_E_WORKSPACE
+    assert _rule(L=500, n=64) == spk.SPK_E_WORKSPACE
+
+
+def test_workspace_sizes():
+    size, back = spk.spk_delta_rule_workspace_size, spk.spk_delta_rule_backward_workspace_size
+    assert size(0, 2, 1, 1, 2, 64, 64) == 0  # a few samples run one after another
+    assert 0 < size(1, 2, 500, 1, 2, 64, 64) < size(1, 4, 500, 1, 2, 64, 64)
+    assert size(1, 2, 500, 1, 3, 64, 64) > size(1, 2, 500, 1, 1, 64, 64)
+    assert size(5, 2, 500, 1, 2, 64, 64) == 0 and size(0, 2, 500, 2, 3, 64, 64) == 0
+    # the states of every chunk, twice, and two rows a sample
+    assert back(0, 1, 320, 1, 1, 64, 64) >= 4 * (2 * 10 * 64 * 64 + 2 * 320 * 64)
+    assert back(0, 0, 320, 1, 1, 64, 64) == 0 and back(0, 1, 0, 1, 1, 64, 64) == 0
