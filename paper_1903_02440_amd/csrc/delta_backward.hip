@@ -24,125 +24,168 @@
 namespace spk {
 namespace delta {
 
+template <class E, int DS>
+struct RscanLds {
+    using F = Blob<E, DS, true>;
+    static constexpr int HEADP = F::HEAD - F::T;  // coefficients, T^T, P^T
+    static constexpr int EARLY = F::K + HEADP, LATE = 2 * F::KT;
+    static constexpr int NBUF = 2 * EARLY + LATE <= LDS_BYTES ? 2 : 1, BYTES = NBUF * EARLY + LATE;
+};
+
 // Grid and columns as the states' kernel (delta_kernels.hpp), chunks from last
-// to first; a wave carries 16 columns of dS.
+// to first; a wave carries 16 columns of dS.  K, T^T, P^T and the coefficients
+// are needed from the start of a chunk, K^T and Q^T in its second half only: with
+// NBUF = 2 the former have two buffers and come during the chunk before, the
+// latter one and come during the first half (what fits the LDS).
 template <class E, int DS, int NBUF>
 __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out, Args a,
                                                      const int32_t *__restrict__ lengths, int compute, Chunks w,
                                                      Kept kept, const float *d_last, float *d_first) {
     using F = Blob<E, DS, true>;
     constexpr int C = F::C, MT = F::MT, NT = F::NT, GP = F::GP;
-    constexpr int HEADP = F::HEAD - F::T, ONE = F::KEY + HEADP;  // coefficients, T^T, P^T
+    using R = RscanLds<E, DS>;
     extern __shared__ char lds[];
     const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, gr = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
-    const int b = blockIdx.x / a.Hv, h = blockIdx.x % a.Hv, hk = h / (a.Hv / a.Hk);
+    const int bh = head_of(blockIdx.x, gridDim.x), b = bh / a.Hv, h = bh % a.Hv, hk = h / (a.Hv / a.Hk);
     const int n = lengths ? max(0, min(a.L, lengths[b])) : a.L, nc = (n + C - 1) / C;
     const int col = ((int)blockIdx.y * compute + wv) * 16 + m;
     const bool mine = wv < compute && col - m < kept.dvp, live = mine && col < a.dv;
-    const int64_t s0 = (int64_t)blockIdx.x * a.dk * a.dv + col;
+    const int64_t s0 = (int64_t)bh * a.dk * a.dv + col;
     const char *key = w.key + ((int64_t)b * a.Hk + hk) * w.NC * F::KEY;
-    const char *head = w.head + (int64_t)blockIdx.x * w.NC * F::HEAD + F::T;
+    const char *head = w.head + (int64_t)bh * w.NC * F::HEAD + F::T;
     f32x4 S[2 * DS];
 #pragma unroll
-    for (int t = 0; t < 2 * DS; ++t)
+    for (int t = 0; t < 2 * DS; ++t) S[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    if (d_last) {
+        const float *from = d_last + (int64_t)bh * a.dk * a.dv + min(col, a.dv - 1);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int d = 16 * t + 4 * gr + r;
-            S[t][r] = live && d < a.dk && d_last ? d_last[s0 + (int64_t)d * a.dv] : 0.0f;
-        }
-    auto fetch = [&](int c) {
-        char *dst = lds + (c % NBUF) * ONE;
-        to_lds(dst, key + (int64_t)c * F::KEY, F::KEY, wv, waves, lane);
-        to_lds(dst + F::KEY, head + (int64_t)c * F::HEAD, HEADP, wv, waves, lane);
+        for (int t = 0; t < 2 * DS; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[t][r] = from[(int64_t)min(16 * t + 4 * gr + r, a.dk - 1) * a.dv];
+#pragma unroll
+        for (int t = 0; t < 2 * DS; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[t][r] = live && 16 * t + 4 * gr + r < a.dk ? S[t][r] : 0.0f;
+    }
+    char *late = lds + NBUF * R::EARLY;
+    auto fetch_early = [&](int c) {
+        char *dst = lds + (c % NBUF) * R::EARLY;
+        to_lds(dst, key + (int64_t)c * F::KEY, F::K, wv, waves, lane);
+        to_lds(dst + F::K, head + (int64_t)c * F::HEAD, R::HEADP, wv, waves, lane);
     };
+    auto fetch_late = [&](int c) { to_lds(late, key + (int64_t)c * F::KEY + F::K, R::LATE, wv, waves, lane); };
     const int64_t vstep = (int64_t)a.Hv * a.dv;
-    const int64_t v0 = ((int64_t)b * a.L * a.Hv + h) * a.dv + col;
-    if (NBUF == 2 && nc) fetch(nc - 1);
+    const E *ocol = d_out + ((int64_t)b * a.L * a.Hv + h) * a.dv + min(col, a.dv - 1);
+    E on[MT][4];
+    auto upstream = [&](int c) {  // (clamped, not skipped: loads behind a branch would each be waited for)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) on[mt][r] = ocol[min(c * C + 16 * mt + 4 * gr + r, n - 1) * vstep];
+    };
+    if (nc) {
+        upstream(nc - 1);
+        fetch_early(nc - 1);
+        if (NBUF == 1) fetch_late(nc - 1);
+        wait_copies();
+    }
+    __syncthreads();
     for (int c = nc - 1; c >= 0; --c) {
-        if (NBUF == 1) {
-            if (c < nc - 1) __syncthreads();
-            fetch(c);
-        }
         float o[MT][4];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = c * C + 16 * mt + 4 * gr + r;
-                o[mt][r] = live && i < n ? to_float(d_out[v0 + i * vstep]) : 0.0f;
-            }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (NBUF == 2 && c > 0) fetch(c - 1);
-        if (!mine) continue;
-        const char *K = lds + (c % NBUF) * ONE, *KT = K + F::K, *QT = KT + F::KT, *H = K + F::KEY;
+            for (int r = 0; r < 4; ++r)
+                o[mt][r] = live && c * C + 16 * mt + 4 * gr + r < n ? to_float(on[mt][r]) : 0.0f;
+        if (c > 0) upstream(c - 1);
+        if (NBUF == 2) fetch_late(c);
+        const char *K = lds + (c % NBUF) * R::EARLY, *H = K + F::K, *KT = late, *QT = late + F::KT;
         const char *TT = H + (F::TTAT - F::T), *PT = H + (F::PAT - F::T);
         const float *co = reinterpret_cast<const float *>(H);
-        float *dst = kept.dS + ((int64_t)blockIdx.x * w.NC + c) * 32 * DS * kept.dvp + col;
+        f32x4 Y[MT];
+        if (mine) {
+            float *dst = kept.dS + ((int64_t)bh * w.NC + c) * 32 * DS * kept.dvp + col;
 #pragma unroll
-        for (int t = 0; t < 2 * DS; ++t)
+            for (int t = 0; t < 2 * DS; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) dst[(int64_t)(16 * t + 4 * gr + r) * kept.dvp] = S[t][r];
-        f32x4 X[MT], Z[MT], Y[MT];
+                for (int r = 0; r < 4; ++r) dst[(int64_t)(16 * t + 4 * gr + r) * kept.dvp] = S[t][r];
+            f32x4 X[MT], Z[MT];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) X[mt] = Z[mt] = Y[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            for (int mt = 0; mt < MT; ++mt) X[mt] = Z[mt] = Y[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < DS; ++s) {
-            const Terms<3> st = split<3>(S[2 * s], S[2 * s + 1]);
+            for (int s = 0; s < DS; ++s) {
+                const Terms<3> st = split<3>(S[2 * s], S[2 * s + 1]);
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) mma<NT, 3>(X[mt], frag<NT>(K + (mt * DS + s) * NT * FRAG, lane), st);
+                for (int mt = 0; mt < MT; ++mt) mma<NT, 3>(X[mt], frag<NT>(K + (mt * DS + s) * NT * FRAG, lane), st);
+            }
+#pragma unroll
+            for (int gp = 0; gp < GP; ++gp) {
+                float x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = o[2 * gp + (j >> 2)][j & 3];
+                const Terms<NT> ot = split<NT>(x);
+#pragma unroll
+                for (int mt = 0; mt <= 2 * gp + 1; ++mt) mma<3, NT>(Z[mt], frag<3>(PT + F::upper(mt, gp) * 3 * FRAG, lane), ot);
+            }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                const f32x4 la = *reinterpret_cast<const f32x4 *>(co + 2 * C + 16 * mt + 4 * gr);
+                X[mt] = la * X[mt] + a.scale * Z[mt];  // dU
+            }
+#pragma unroll
+            for (int gp = 0; gp < GP; ++gp) {
+                const Terms<3> ut = split<3>(X[2 * gp], X[2 * gp + 1]);
+#pragma unroll
+                for (int mt = 0; mt <= 2 * gp + 1; ++mt) mma<3, 3>(Y[mt], frag<3>(TT + F::upper(mt, gp) * 3 * FRAG, lane), ut);
+            }
         }
-#pragma unroll
-        for (int gp = 0; gp < GP; ++gp) {
-            float x[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = o[2 * gp + (j >> 2)][j & 3];
-            const Terms<NT> ot = split<NT>(x);
-#pragma unroll
-            for (int mt = 0; mt <= 2 * gp + 1; ++mt) mma<3, NT>(Z[mt], frag<3>(PT + F::upper(mt, gp) * 3 * FRAG, lane), ot);
+        if (NBUF == 2) {
+            wait_copies();
+            __syncthreads();
+            if (c > 0) fetch_early(c - 1);
         }
+        if (mine) {
+            float *yd = kept.Y + ((int64_t)bh * w.NC + c) * C * kept.dvp + col;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            const f32x4 la = *reinterpret_cast<const f32x4 *>(co + 2 * C + 16 * mt + 4 * gr);
-            X[mt] = la * X[mt] + a.scale * Z[mt];  // dU
-        }
+            for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int gp = 0; gp < GP; ++gp) {
-            const Terms<3> ut = split<3>(X[2 * gp], X[2 * gp + 1]);
+                for (int r = 0; r < 4; ++r) yd[(int64_t)(16 * mt + 4 * gr + r) * kept.dvp] = Y[mt][r];
+            const float end = co[C - 1];
 #pragma unroll
-            for (int mt = 0; mt <= 2 * gp + 1; ++mt) mma<3, 3>(Y[mt], frag<3>(TT + F::upper(mt, gp) * 3 * FRAG, lane), ut);
-        }
-        float *yd = kept.Y + ((int64_t)blockIdx.x * w.NC + c) * C * kept.dvp + col;
+            for (int t = 0; t < 2 * DS; ++t)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+                for (int r = 0; r < 4; ++r) S[t][r] *= end;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) yd[(int64_t)(16 * mt + 4 * gr + r) * kept.dvp] = Y[mt][r];
-        const float end = co[C - 1];
+            for (int gp = 0; gp < GP; ++gp) {
+                float x[8], y[8];
 #pragma unroll
-        for (int t = 0; t < 2 * DS; ++t)
+                for (int hf = 0; hf < 2; ++hf) {
+                    const f32x4 ev = *reinterpret_cast<const f32x4 *>(co + 32 * gp + 16 * hf + 4 * gr);
+                    const f32x4 be = *reinterpret_cast<const f32x4 *>(co + C + 32 * gp + 16 * hf + 4 * gr);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) S[t][r] *= end;
+                    for (int r = 0; r < 4; ++r) {
+                        x[4 * hf + r] = a.scale * ev[r] * o[2 * gp + hf][r];
+                        y[4 * hf + r] = -be[r] * ev[r] * Y[2 * gp + hf][r];
+                    }
+                }
+                const Terms<3> xt = split<3>(x), yt = split<3>(y);
 #pragma unroll
-        for (int gp = 0; gp < GP; ++gp) {
-            float x[8], y[8];
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-                const f32x4 ev = *reinterpret_cast<const f32x4 *>(co + 32 * gp + 16 * hf + 4 * gr);
-                const f32x4 be = *reinterpret_cast<const f32x4 *>(co + C + 32 * gp + 16 * hf + 4 * gr);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    x[4 * hf + r] = a.scale * ev[r] * o[2 * gp + hf][r];
-                    y[4 * hf + r] = -be[r] * ev[r] * Y[2 * gp + hf][r];
+                for (int t = 0; t < 2 * DS; ++t) {
+                    mma<NT, 3>(S[t], frag<NT>(QT + (t * GP + gp) * NT * FRAG, lane), xt);
+                    mma<NT, 3>(S[t], frag<NT>(KT + (t * GP + gp) * NT * FRAG, lane), yt);
                 }
             }
-            const Terms<3> xt = split<3>(x), yt = split<3>(y);
-#pragma unroll
-            for (int t = 0; t < 2 * DS; ++t) {
-                mma<NT, 3>(S[t], frag<NT>(QT + (t * GP + gp) * NT * FRAG, lane), xt);
-                mma<NT, 3>(S[t], frag<NT>(KT + (t * GP + gp) * NT * FRAG, lane), yt);
+        }
+        if (NBUF == 1) {
+            __syncthreads();
+            if (c > 0) {
+                fetch_early(c - 1);
+                fetch_late(c - 1);
             }
         }
+        wait_copies();
+        __syncthreads();
     }
     if (!live || !d_first) return;
 #pragma unroll
@@ -241,25 +284,28 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
 #pragma unroll
                     for (int r = 0; r < 4; ++r) x[r] = x0[r], x[4 + r] = x1[r];
                     put_frag<3>((which ? fu : fy) + mt * 3 * FRAG, lane, split<3>(x));
-                    if (which == 0 && i < n) {
-                        const int64_t vrow = ((row0 + i) * a.Hv + h) * a.dv;
+                    if (which == 0) {
+                        const int64_t vrow = ((row0 + min(i, n - 1)) * a.Hv + h) * a.dv;
                         const float be = co[C + i];
+                        E ve[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) ve[j] = v[vrow + min(32 * vg + slot(gr, j), a.dv - 1)];
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
                             const int cv = 32 * vg + slot(gr, j);
-                            if (cv < a.dv) {
-                                yvp += x[j] * to_float(v[vrow + cv]);
-                                d_v[vrow + cv] = from_float<E>(be * x[j]);
-                            }
+                            const bool in = i < n && cv < a.dv;
+                            yvp += in ? x[j] * to_float(ve[j]) : 0.0f;
+                            if (in) d_v[vrow + cv] = from_float<E>(be * x[j]);
                         }
                     }
                 } else {
-                    const int64_t vrow = ((row0 + i) * a.Hv + h) * a.dv;
+                    const int64_t vrow = ((row0 + min(i, n - 1)) * a.Hv + h) * a.dv;
+                    E oe[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int cv = 32 * vg + slot(gr, j);
-                        x[j] = i < n && cv < a.dv ? to_float(d_out[vrow + cv]) : 0.0f;
-                    }
+                    for (int j = 0; j < 8; ++j) oe[j] = d_out[vrow + min(32 * vg + slot(gr, j), a.dv - 1)];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        x[j] = i < n && 32 * vg + slot(gr, j) < a.dv ? to_float(oe[j]) : 0.0f;
                     put_frag<NT>(fo + mt * NT * FRAG, lane, split<NT>(x));
                 }
             }
@@ -340,6 +386,15 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
         for (int p = 0; p < TW; ++p) {
             const int t = p * GRAD_WAVES + wv, d = 16 * t + m;
             if (t >= 2 * DS) continue;
+            E ke[MT][4], qe[MT][4];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int64_t at = ((row0 + min(16 * mt + 4 * gr + r, n - 1)) * a.Hk + hk) * a.dk + min(d, a.dk - 1);
+                    ke[mt][r] = k[at];
+                    qe[mt][r] = q[at];
+                }
             Terms<NT> kt[GP], qt[GP];
 #pragma unroll
             for (int gp = 0; gp < GP; ++gp) {
@@ -355,11 +410,9 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
                 float kk[4], qq[4];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int i = 16 * mt + 4 * gr + r;
-                    const int64_t at = ((row0 + i) * a.Hk + hk) * a.dk + d;
-                    const bool in = i < n && d < a.dk;
-                    kk[r] = in ? to_float(k[at]) : 0.0f;
-                    qq[r] = in ? to_float(q[at]) : 0.0f;
+                    const bool in = 16 * mt + 4 * gr + r < n && d < a.dk;
+                    kk[r] = in ? to_float(ke[mt][r]) : 0.0f;
+                    qq[r] = in ? to_float(qe[mt][r]) : 0.0f;
                     pe += kk[r] * z[r];
                 }
                 f32x4 mk = {0.f, 0.f, 0.f, 0.f}, mc = mk;
@@ -488,9 +541,10 @@ int backward(const Call &c, const Args &a, void *ws, hipStream_t st, const char 
     constexpr int NB = 2 * F::SCAN <= LDS_BYTES ? 2 : 1;
     hipLaunchKernelGGL((k_delta_scan<E, DS, NB, true>), cols, threads, NB * F::SCAN, st, v, a, c.lengths, compute, w,
                        c.state_in, (E *)nullptr, (float *)nullptr, kept);
-    constexpr int ONE = F::KEY + F::HEAD - F::T, NR = 2 * ONE <= LDS_BYTES ? 2 : 1;
-    static_assert(ONE <= LDS_BYTES && F::SCAN <= LDS_BYTES && LP <= LDS_BYTES && LG <= LDS_BYTES, "LDS");
-    hipLaunchKernelGGL((k_delta_rscan<E, DS, NR>), cols, threads, NR * ONE, st, d_out, a, c.lengths, compute, w, kept,
+    using R = RscanLds<E, DS>;
+    constexpr int LR = R::BYTES, NR = R::NBUF;
+    static_assert(LR <= LDS_BYTES && F::SCAN <= LDS_BYTES && LP <= LDS_BYTES && LG <= LDS_BYTES, "LDS");
+    hipLaunchKernelGGL((k_delta_rscan<E, DS, NR>), cols, threads, LR, st, d_out, a, c.lengths, compute, w, kept,
                        c.d_last, c.d_first);
     hipLaunchKernelGGL((k_delta_grads<E, DS>), per_key, dim3(GRAD_THREADS), LG, st, q, k, v, c.g, d_out, a, c.lengths, w, kept, static_cast<E *>(c.d_q), static_cast<E *>(c.d_k),
                        static_cast<E *>(c.d_v), c.d_g, c.d_beta);

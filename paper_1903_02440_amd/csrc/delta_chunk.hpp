@@ -148,13 +148,24 @@ constexpr int chunk_of(int dtype) { return dtype == SPK_F32 ? 32 : 64; }
 // exponential is 0, so that differences of sums stay defined.
 __device__ __forceinline__ double log_decay(float g) { return g < -1e4f ? -1e4 : (double)g; }
 
-// Copies n bytes (a multiple of 1 KiB) to LDS, past the registers; both ends
-// 16-byte aligned.  All waves of the workgroup take part; wait for vmcnt(0)
-// and a barrier before use.
+// Copies n bytes (a multiple of 1 KiB) to LDS past the registers; both ends
+// 16-byte aligned.  All waves of the workgroup take part.  The copy is one the
+// compiler does not count: before use, wait for vmcnt(0) and then a barrier.
+// (As a builtin it would make every LDS read wait for it, also those of another
+// buffer.)
 __device__ __forceinline__ void to_lds(char *dst, const char *src, int n, int wave, int waves, int lane) {
+    const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)dst;
     for (int o = wave * FRAG; o < n; o += waves * FRAG)
-        __builtin_amdgcn_global_load_lds(reinterpret_cast<const u32x4 *>(src + o) + lane,
-                                         reinterpret_cast<u32x4 *>(dst + o), 16, 0, 0);
+        asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(src + o + lane * 16),
+                     "{m0}"(__builtin_amdgcn_readfirstlane((int)(at + o)))
+                     : "memory");
+}
+// All of the wave's copies and loads have arrived, its stores are out.  (As a
+// builtin the compiler counts it too: loads before it need no wait of their own.)
+__device__ __forceinline__ void wait_copies() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+    asm volatile("" ::: "memory");
 }
 
 }  // namespace delta

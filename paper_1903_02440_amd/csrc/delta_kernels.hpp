@@ -2,10 +2,14 @@
 // the states from chunk to chunk (gfx950).
 #pragma once
 
+#include <type_traits>
+
 #include "delta_chunk.hpp"
 
 namespace spk {
 namespace delta {
+
+constexpr int LDS_BYTES = 160 * 1024;
 
 // What the operand kernel leaves for the others, per (sequence, key head, chunk)
 // and per (sequence, value head, chunk), in bytes:
@@ -38,35 +42,37 @@ struct Kept {
     float *S, *dS, *U, *Y;
 };
 
-// Eight elements of a row of keys or queries, 0 past its end.
+// Eight elements of a row of keys or queries, as two runs of four (32 s + 4 g on
+// and 16 later), in the row's own type.  Indices past the row are clamped and the
+// elements set to 0 by the caller: loads behind a branch would each be waited for.
 template <class E>
-__device__ __forceinline__ void load8(const E *p, int s, int g, int dk, bool wide, float (&x)[8]) {
-    // (elements 0..3 and 4..7 are runs of 4; wide: both are whole and aligned)
-    const int c0 = 32 * s + 4 * g;
-    if (wide) {
+struct Raw8 {
+    E e[8];
+};
+template <class E, bool WIDE>
+__device__ __forceinline__ Raw8<E> load8(const E *p, int s, int g, int dk) {
+    Raw8<E> r;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int c = c0 + 16 * h;
-            if (c < dk) {
-                if constexpr (sizeof(E) == 4) {
-                    const float4 w = *reinterpret_cast<const float4 *>(p + c);
-                    x[4 * h] = w.x, x[4 * h + 1] = w.y, x[4 * h + 2] = w.z, x[4 * h + 3] = w.w;
-                } else {
-                    const uint2 w = *reinterpret_cast<const uint2 *>(p + c);
-                    x[4 * h] = __uint_as_float(w.x << 16), x[4 * h + 1] = __uint_as_float(w.x & 0xFFFF0000u);
-                    x[4 * h + 2] = __uint_as_float(w.y << 16), x[4 * h + 3] = __uint_as_float(w.y & 0xFFFF0000u);
-                }
-            } else {
-                x[4 * h] = x[4 * h + 1] = x[4 * h + 2] = x[4 * h + 3] = 0.0f;
-            }
-        }
-    } else {
+    for (int h = 0; h < 2; ++h) {
+        const int c = 32 * s + 4 * g + 16 * h;
+        if constexpr (WIDE) {  // dk a multiple of 4, rows aligned to four elements
+            struct alignas(4 * sizeof(E)) Four {
+                E e[4];
+            };
+            const Four w = *reinterpret_cast<const Four *>(p + min(c, dk - 4));
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int c = 32 * s + slot(g, j);
-            x[j] = c < dk ? to_float(p[c]) : 0.0f;
+            for (int j = 0; j < 4; ++j) r.e[4 * h + j] = w.e[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r.e[4 * h + j] = p[min(c + j, dk - 1)];
         }
     }
+    return r;
+}
+template <class E>
+__device__ __forceinline__ void as_floats(const Raw8<E> &w, int s, int g, int dk, bool row, float (&x)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = row && 32 * s + slot(g, j) < dk ? to_float(w.e[j]) : 0.0f;
 }
 
 constexpr int PREP_THREADS = 256;
@@ -121,18 +127,33 @@ __global__ __launch_bounds__(PREP_THREADS) void k_delta_prep(const E *__restrict
     float *bet = reinterpret_cast<float *>(gam + C);
     char *key = w.key + ((int64_t)blockIdx.y * w.NC + chunk) * F::KEY;
 
-    // K and Q
-    for (int u = tid; u < 2 * MT * DS * 64; u += PREP_THREADS) {
-        const int f = u >> 6, mt = f / DS % MT, s = f % DS;  // (lane = u & 63)
-        const bool isq = f >= MT * DS;
-        const int i = 16 * mt + m;
-        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (i < n) load8<E>((isq ? q : k) + (((int64_t)b * a.L + chunk * C + i) * a.Hk + hk) * a.dk, s, gr, a.dk, wide, x);
-        const Terms<NT> t = split<NT>(x);
-        const int o = (mt * DS + s) * NT * FRAG;
-        put_frag<NT>((isq ? fq : fk) + o, lane, t);
-        if (!isq || !BWD) put_frag<NT>(key + (isq ? F::K + F::KT : 0) + o, lane, t);
-    }
+    // K and Q: four units of a thread at a time, so that their loads overlap
+    auto units = [&](auto wd) {
+        constexpr int NU = 2 * MT * DS * 64 / PREP_THREADS, UB = NU < 4 ? NU : 4;
+        for (int u0 = tid; u0 < NU * PREP_THREADS; u0 += UB * PREP_THREADS) {
+            Raw8<E> raw[UB];
+#pragma unroll
+            for (int x = 0; x < UB; ++x) {
+                const int f = (u0 + x * PREP_THREADS) >> 6, mt = f / DS % MT, s = f % DS;  // (lane = unit & 63)
+                const int i = min(16 * mt + m, n - 1);
+                raw[x] = load8<E, decltype(wd)::value>(
+                    (f >= MT * DS ? q : k) + (((int64_t)b * a.L + chunk * C + i) * a.Hk + hk) * a.dk, s, gr, a.dk);
+            }
+#pragma unroll
+            for (int x = 0; x < UB; ++x) {
+                const int f = (u0 + x * PREP_THREADS) >> 6, mt = f / DS % MT, s = f % DS;
+                const bool isq = f >= MT * DS;
+                float y[8];
+                as_floats(raw[x], s, gr, a.dk, 16 * mt + m < n, y);
+                const Terms<NT> t = split<NT>(y);
+                const int o = (mt * DS + s) * NT * FRAG;
+                put_frag<NT>((isq ? fq : fk) + o, lane, t);
+                if (!isq || !BWD) put_frag<NT>(key + (isq ? F::K + F::KT : 0) + o, lane, t);
+            }
+        }
+    };
+    if (wide) units(std::true_type{});
+    else units(std::false_type{});
     __syncthreads();
     // K^T (and Q^T): row d = 16 t + m, samples slot(gr, j) of group gp
     constexpr int TF = 2 * DS * GP * NT;
@@ -273,6 +294,10 @@ __global__ __launch_bounds__(PREP_THREADS) void k_delta_prep(const E *__restrict
     }
 }
 
+// Workgroups go to the eight XCDs in turn; this order puts the value heads of a
+// key head, which read the same operands, on one XCD's L2.
+__device__ __forceinline__ int head_of(int x, int n) { return n % 8 == 0 ? (x & 7) * (n >> 3) + (x >> 3) : x; }
+
 // Grid (b * Hv + value head, block of columns): a wave carries 16 columns of the
 // state through the chunks, in registers: as the right operand of K S and Q S
 // (three terms) and as the sums of K^T (last U).  The waves of a workgroup share
@@ -290,21 +315,27 @@ __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Arg
     extern __shared__ char lds[];
     const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, gr = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
-    const int b = blockIdx.x / a.Hv, h = blockIdx.x % a.Hv, hk = h / (a.Hv / a.Hk);
+    const int bh = head_of(blockIdx.x, gridDim.x), b = bh / a.Hv, h = bh % a.Hv, hk = h / (a.Hv / a.Hk);
     const int n = lengths ? max(0, min(a.L, lengths[b])) : a.L, nc = (n + C - 1) / C;
     const int col = ((int)blockIdx.y * compute + wv) * 16 + m;
     const bool mine = wv < compute && col - m < (STATES ? kept.dvp : a.dv), live = mine && col < a.dv;
-    const int64_t s0 = (int64_t)blockIdx.x * a.dk * a.dv + col;
+    const int64_t s0 = (int64_t)bh * a.dk * a.dv + col;
     const char *key = w.key + ((int64_t)b * a.Hk + hk) * w.NC * F::KEY;
-    const char *head = w.head + (int64_t)blockIdx.x * w.NC * F::HEAD;
+    const char *head = w.head + (int64_t)bh * w.NC * F::HEAD;
     f32x4 S[2 * DS];
 #pragma unroll
-    for (int t = 0; t < 2 * DS; ++t)
+    for (int t = 0; t < 2 * DS; ++t) S[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    if (state_in) {
+        const float *from = state_in + (int64_t)bh * a.dk * a.dv + min(col, a.dv - 1);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int d = 16 * t + 4 * gr + r;
-            S[t][r] = live && d < a.dk && state_in ? state_in[s0 + (int64_t)d * a.dv] : 0.0f;
-        }
+        for (int t = 0; t < 2 * DS; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[t][r] = from[(int64_t)min(16 * t + 4 * gr + r, a.dk - 1) * a.dv];
+#pragma unroll
+        for (int t = 0; t < 2 * DS; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[t][r] = live && 16 * t + 4 * gr + r < a.dk ? S[t][r] : 0.0f;
+    }
     auto fetch = [&](int c) {
         char *dst = lds + (c % NBUF) * F::SCAN;
         to_lds(dst, key + (int64_t)c * F::KEY, F::SCAN_KEY, wv, waves, lane);
@@ -312,100 +343,124 @@ __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Arg
     };
     const int64_t vstep = (int64_t)a.Hv * a.dv;
     const int64_t v0 = ((int64_t)b * a.L * a.Hv + h) * a.dv + col;
-    if (NBUF == 2 && nc) fetch(0);
-    for (int c = 0; c < nc; ++c) {
-        if (NBUF == 1) {
-            if (c) __syncthreads();
-            fetch(c);
-        }
-        float vv[MT][4];
+    const E *vcol = v + ((int64_t)b * a.L * a.Hv + h) * a.dv + min(col, a.dv - 1);
+    E vv[MT][4];
+    auto values = [&](int c) {  // (clamped, not skipped: loads behind a branch would each be waited for)
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = c * C + 16 * mt + 4 * gr + r;
-                vv[mt][r] = live && i < n ? to_float(v[v0 + i * vstep]) : 0.0f;
-            }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (NBUF == 2 && c + 1 < nc) fetch(c + 1);
-        if (!mine) continue;
-        const char *K = lds + (c % NBUF) * F::SCAN, *KT = K + F::K, *Q = KT + F::KT, *T = K + F::SCAN_KEY,
-                   *P = T + F::PAT;
-        const float *co = reinterpret_cast<const float *>(T + F::T);
-        if (STATES) {
-            float *dst = kept.S + ((int64_t)blockIdx.x * w.NC + c) * 32 * DS * kept.dvp + col;
+            for (int r = 0; r < 4; ++r) vv[mt][r] = vcol[min(c * C + 16 * mt + 4 * gr + r, n - 1) * vstep];
+    };
+    if (nc) {
+        values(0);
+        fetch(0);
+        wait_copies();
+    }
+    __syncthreads();
+    for (int c = 0; c < nc; ++c) {
+        float vc[MT][4];
 #pragma unroll
-            for (int t = 0; t < 2 * DS; ++t)
+        for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) dst[(int64_t)(16 * t + 4 * gr + r) * kept.dvp] = S[t][r];
+            for (int r = 0; r < 4; ++r)
+                vc[mt][r] = live && c * C + 16 * mt + 4 * gr + r < n ? to_float(vv[mt][r]) : 0.0f;
+        if (c + 1 < nc) {
+            values(c + 1);
+            if (NBUF == 2) fetch(c + 1);
         }
-        f32x4 X[MT], Y[MT];
+        f32x4 Y[MT];
+        if (mine) {
+            const char *K = lds + (c % NBUF) * F::SCAN, *KT = K + F::K, *Q = KT + F::KT, *T = K + F::SCAN_KEY,
+                       *P = T + F::PAT;
+            const float *co = reinterpret_cast<const float *>(T + F::T);
+            if (STATES) {
+                float *dst = kept.S + ((int64_t)bh * w.NC + c) * 32 * DS * kept.dvp + col;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) X[mt] = Y[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+                for (int t = 0; t < 2 * DS; ++t)
 #pragma unroll
-        for (int s = 0; s < DS; ++s) {
-            const Terms<3> st = split<3>(S[2 * s], S[2 * s + 1]);
-            Terms<NP> sp;
+                    for (int r = 0; r < 4; ++r) dst[(int64_t)(16 * t + 4 * gr + r) * kept.dvp] = S[t][r];
+            }
+            f32x4 X[MT];
 #pragma unroll
-            for (int i = 0; i < NP; ++i) sp.t[i] = st.t[i];
+            for (int mt = 0; mt < MT; ++mt) X[mt] = Y[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < DS; ++s) {
+                const Terms<3> st = split<3>(S[2 * s], S[2 * s + 1]);
+                Terms<NP> sp;
+#pragma unroll
+                for (int i = 0; i < NP; ++i) sp.t[i] = st.t[i];
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    mma<NT, 3>(X[mt], frag<NT>(K + (mt * DS + s) * NT * FRAG, lane), st);
+                    if (!STATES) mma<NT, NP>(Y[mt], frag<NT>(Q + (mt * DS + s) * NT * FRAG, lane), sp);
+                }
+            }
+            f32x4 U[MT];
+            float e[MT][4];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
-                mma<NT, 3>(X[mt], frag<NT>(K + (mt * DS + s) * NT * FRAG, lane), st);
-                if (!STATES) mma<NT, NP>(Y[mt], frag<NT>(Q + (mt * DS + s) * NT * FRAG, lane), sp);
+                const f32x4 ev = *reinterpret_cast<const f32x4 *>(co + 16 * mt + 4 * gr);
+                const f32x4 be = *reinterpret_cast<const f32x4 *>(co + C + 16 * mt + 4 * gr);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    e[mt][r] = ev[r];
+                    X[mt][r] = be[r] * (vc[mt][r] - ev[r] * X[mt][r]);
+                }
+                U[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
             }
-        }
-        f32x4 U[MT];
-        float e[MT][4];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            const f32x4 ev = *reinterpret_cast<const f32x4 *>(co + 16 * mt + 4 * gr);
-            const f32x4 be = *reinterpret_cast<const f32x4 *>(co + C + 16 * mt + 4 * gr);
+            for (int gp = 0; gp < GP; ++gp) {
+                const Terms<3> rt = split<3>(X[2 * gp], X[2 * gp + 1]);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                e[mt][r] = ev[r];
-                X[mt][r] = be[r] * (vv[mt][r] - ev[r] * X[mt][r]);
+                for (int mt = 2 * gp; mt < MT; ++mt) mma<3, 3>(U[mt], frag<3>(T + F::lower(mt, gp) * 3 * FRAG, lane), rt);
             }
-            U[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
-        }
 #pragma unroll
-        for (int gp = 0; gp < GP; ++gp) {
-            const Terms<3> rt = split<3>(X[2 * gp], X[2 * gp + 1]);
+            for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int mt = 2 * gp; mt < MT; ++mt) mma<3, 3>(U[mt], frag<3>(T + F::lower(mt, gp) * 3 * FRAG, lane), rt);
-        }
+                for (int r = 0; r < 4; ++r) Y[mt][r] *= STATES ? 1.0f : e[mt][r];
+            if (STATES) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) Y[mt][r] *= e[mt][r];
-        const float end = co[C - 1];  // E of the last sample
-#pragma unroll
-        for (int t = 0; t < 2 * DS; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) S[t][r] *= end;
-#pragma unroll
-        for (int gp = 0; gp < GP; ++gp) {
-            if (!STATES) {
-                const Terms<NP> ut = split<NP>(U[2 * gp], U[2 * gp + 1]);
-#pragma unroll
-                for (int mt = 2 * gp; mt < MT; ++mt)
-                    mma<NP, NP>(Y[mt], frag<NP>(P + F::lower(mt, gp) * NP * FRAG, lane), ut);
+                for (int mt = 0; mt < MT; ++mt) Y[mt] = U[mt];
             }
-            const f32x4 l0 = *reinterpret_cast<const f32x4 *>(co + 2 * C + 32 * gp + 4 * gr);
-            const f32x4 l1 = *reinterpret_cast<const f32x4 *>(co + 2 * C + 32 * gp + 16 + 4 * gr);
-            const Terms<3> lt = split<3>(U[2 * gp] * l0, U[2 * gp + 1] * l1);
+            const float end = co[C - 1];  // E of the last sample
 #pragma unroll
             for (int t = 0; t < 2 * DS; ++t)
-                mma<NT, 3>(S[t], frag<NT>(KT + (t * GP + gp) * NT * FRAG, lane), lt);
-        }
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+                for (int r = 0; r < 4; ++r) S[t][r] *= end;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = c * C + 16 * mt + 4 * gr + r;
-                if (STATES) kept.U[((int64_t)blockIdx.x * w.NC * C + i) * kept.dvp + col] = U[mt][r];
-                else if (live && i < n) out[v0 + i * vstep] = from_float<E>(a.scale * Y[mt][r]);
+            for (int gp = 0; gp < GP; ++gp) {
+                if (!STATES) {
+                    const Terms<NP> ut = split<NP>(U[2 * gp], U[2 * gp + 1]);
+#pragma unroll
+                    for (int mt = 2 * gp; mt < MT; ++mt)
+                        mma<NP, NP>(Y[mt], frag<NP>(P + F::lower(mt, gp) * NP * FRAG, lane), ut);
+                }
+                const f32x4 l0 = *reinterpret_cast<const f32x4 *>(co + 2 * C + 32 * gp + 4 * gr);
+                const f32x4 l1 = *reinterpret_cast<const f32x4 *>(co + 2 * C + 32 * gp + 16 + 4 * gr);
+                const Terms<3> lt = split<3>(U[2 * gp] * l0, U[2 * gp + 1] * l1);
+#pragma unroll
+                for (int t = 0; t < 2 * DS; ++t)
+                    mma<NT, 3>(S[t], frag<NT>(KT + (t * GP + gp) * NT * FRAG, lane), lt);
             }
+        }
+        // the next chunk's operands have come; what is stored now has a chunk's time to get out
+        if (NBUF == 2) wait_copies();
+        __syncthreads();
+        if (NBUF == 1 && c + 1 < nc) fetch(c + 1);
+        if (mine) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = c * C + 16 * mt + 4 * gr + r;
+                    if (STATES) kept.U[((int64_t)bh * w.NC * C + i) * kept.dvp + col] = Y[mt][r];
+                    else if (live && i < n) out[v0 + i * vstep] = from_float<E>(a.scale * Y[mt][r]);
+                }
+        }
+        if (NBUF == 1) {
+            wait_copies();
+            __syncthreads();
+        }
     }
     if (!live || !state_out) return;
 #pragma unroll
@@ -416,8 +471,6 @@ __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Arg
             if (d < a.dk) state_out[s0 + (int64_t)d * a.dv] = S[t][r];
         }
 }
-
-constexpr int LDS_BYTES = 160 * 1024;
 
 // Waves of a workgroup that carry columns, for `tiles` of 16 columns a head: up
 // to eight share the operands, fewer where the workgroups would not fill the CUs.
