@@ -50,7 +50,7 @@ enum { SPK_F32 = 0, SPK_BF16 = 1 };
  * All sums and states are held in float; bfloat16 inputs are exact terms of
  * the products.  Repeated calls give the same bits.
  * Limits: 1 <= dk <= 256, 1 <= dv <= 4096, Hv a multiple of Hk, B*Hv <= 65535,
- * L <= 2^24.  Workspace: spk_delta_rule_workspace_size(...) bytes.          */
+ * Hv*dv <= 2^22, L <= 2^24.  Workspace: spk_delta_rule_workspace_size(...) bytes.          */
 SPK_API size_t spk_delta_rule_workspace_size(int dtype, int B, int L, int Hk, int Hv, int dk, int dv);
 SPK_API int spk_delta_rule(const void *q, const void *k, const void *v, const float *g, const float *beta, int dtype,
                            int B, int L, int Hk, int Hv, int dk, int dv, float scale, const int32_t *lengths,

@@ -21,6 +21,7 @@ int check(const Args &a, const char *name) {
     SPK_REQUIRE(a.dk <= 256, SPK_E_RANGE, "%s: dk=%d > 256", name, a.dk);
     SPK_REQUIRE(a.dv <= 4096, SPK_E_RANGE, "%s: dv=%d > 4096", name, a.dv);
     SPK_REQUIRE((int64_t)a.B * a.Hv <= 65535, SPK_E_RANGE, "%s: B*Hv above 65535", name);
+    SPK_REQUIRE((int64_t)a.Hv * a.dv <= (1 << 22), SPK_E_RANGE, "%s: Hv*dv above 2^22", name);
     SPK_REQUIRE(a.L <= (1 << 24), SPK_E_RANGE, "%s: L=%d > 2^24", name, a.L);
     SPK_REQUIRE(std::isfinite(a.scale), SPK_E_ARG, "%s: scale must be finite", name);
     return SPK_OK;

@@ -76,13 +76,24 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
     };
     auto fetch_late = [&](int c) { to_lds(late, key + (int64_t)c * F::KEY + F::K, R::LATE, wv, waves, lane); };
     const int64_t vstep = (int64_t)a.Hv * a.dv;
-    const E *ocol = d_out + ((int64_t)b * a.L * a.Hv + h) * a.dv + min(col, a.dv - 1);
+    const E *orow = d_out + ((int64_t)b * a.L * a.Hv + h) * a.dv;
+    const uint32_t lin = (uint32_t)((4 * gr * vstep + min(col, a.dv - 1)) * sizeof(E)),
+                   lkept = (uint32_t)(4 * gr * kept.dvp + col) * 4;
     E on[MT][4];
-    auto upstream = [&](int c) {  // (clamped, not skipped: loads behind a branch would each be waited for)
+    auto upstream = [&](int c) {
+        const E *p = orow + (int64_t)c * C * vstep;
+        if ((c + 1) * C <= n) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+            for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) on[mt][r] = ocol[min(c * C + 16 * mt + 4 * gr + r, n - 1) * vstep];
+                for (int r = 0; r < 4; ++r) on[mt][r] = at(p + (16 * mt + r) * vstep, lin);
+        } else {  // (clamped, not skipped: loads behind a branch would each be waited for)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    on[mt][r] = p[min(16 * mt + 4 * gr + r, n - 1 - c * C) * vstep + min(col, a.dv - 1)];
+        }
     };
     if (nc) {
         upstream(nc - 1);
@@ -105,11 +116,11 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
         const float *co = reinterpret_cast<const float *>(H);
         f32x4 Y[MT];
         if (mine) {
-            float *dst = kept.dS + ((int64_t)bh * w.NC + c) * 32 * DS * kept.dvp + col;
+            float *dst = kept.dS + ((int64_t)bh * w.NC + c) * 32 * DS * kept.dvp;
 #pragma unroll
             for (int t = 0; t < 2 * DS; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) dst[(int64_t)(16 * t + 4 * gr + r) * kept.dvp] = S[t][r];
+                for (int r = 0; r < 4; ++r) at(dst + (16 * t + r) * kept.dvp, lkept) = S[t][r];
             f32x4 X[MT], Z[MT];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) X[mt] = Z[mt] = Y[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -131,7 +142,7 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
                 const f32x4 la = *reinterpret_cast<const f32x4 *>(co + 2 * C + 16 * mt + 4 * gr);
-                X[mt] = la * X[mt] + a.scale * Z[mt];  // dU
+                X[mt] = la * X[mt] + Z[mt];  // dU
             }
 #pragma unroll
             for (int gp = 0; gp < GP; ++gp) {
@@ -146,11 +157,11 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
             if (c > 0) fetch_early(c - 1);
         }
         if (mine) {
-            float *yd = kept.Y + ((int64_t)bh * w.NC + c) * C * kept.dvp + col;
+            float *yd = kept.Y + ((int64_t)bh * w.NC + c) * C * kept.dvp;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) yd[(int64_t)(16 * mt + 4 * gr + r) * kept.dvp] = Y[mt][r];
+                for (int r = 0; r < 4; ++r) at(yd + (16 * mt + r) * kept.dvp, lkept) = Y[mt][r];
             const float end = co[C - 1];
 #pragma unroll
             for (int t = 0; t < 2 * DS; ++t)
@@ -163,9 +174,10 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
                 for (int hf = 0; hf < 2; ++hf) {
                     const f32x4 ev = *reinterpret_cast<const f32x4 *>(co + 32 * gp + 16 * hf + 4 * gr);
                     const f32x4 be = *reinterpret_cast<const f32x4 *>(co + C + 32 * gp + 16 * hf + 4 * gr);
+                    const f32x4 es = *reinterpret_cast<const f32x4 *>(co + 3 * C + 32 * gp + 16 * hf + 4 * gr);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        x[4 * hf + r] = a.scale * ev[r] * o[2 * gp + hf][r];
+                        x[4 * hf + r] = es[r] * o[2 * gp + hf][r];
                         y[4 * hf + r] = -be[r] * ev[r] * Y[2 * gp + hf][r];
                     }
                 }

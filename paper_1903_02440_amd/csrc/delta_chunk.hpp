@@ -6,6 +6,7 @@
 //     (I + A) U = beta (V - E K S)      A_ij = beta_i D_ij k_i . k_j  (j < i)
 //     out       = scale (E Q S + P U)   P_ij = D_ij q_i . k_j         (j <= i)
 //     S        <- E_C S + K^T (last U)
+// (P is kept times the scale.)
 // T = (I + A)^-1, P and the decays depend on the inputs alone, so all chunks
 // make them at once; the states then go through the chunks in order.
 //
@@ -22,6 +23,8 @@
 // the 32.  Fragments are laid out for that order, so results feed the next
 // product without leaving their lane.
 #pragma once
+
+#include <type_traits>
 
 #include "delta.hpp"
 
@@ -97,6 +100,14 @@ __device__ __forceinline__ void mma(f32x4 &c, const Terms<NA> &a, const Terms<NB
             if (o - i >= 0 && o - i < NB) c = mfma(a.t[i], b.t[o - i], c);
 }
 
+// Element at a uniform place p plus the lane's own 32-bit byte offset: the
+// address costs no vector instruction.
+template <class T>
+__device__ __forceinline__ T &at(T *p, uint32_t bytes) {
+    using Byte = typename std::conditional<std::is_const<T>::value, const char, char>::type;
+    return *reinterpret_cast<T *>(reinterpret_cast<Byte *>(p) + bytes);
+}
+
 // The lane's part of a fragment of N terms.
 template <int N>
 __device__ __forceinline__ Terms<N> frag(const char *p, int lane) {
@@ -133,7 +144,7 @@ struct Lay {
     static constexpr int TRI = MT == 4 ? 6 : 2;
     static constexpr int K = MT * DS * NT * FRAG;  // rows of K (or Q), summed over dk: [mt][s][term]
     static constexpr int KT = 2 * DS * GP * NT * FRAG;  // its transpose, summed over the samples: [t][gp][term]
-    static constexpr int COEF = FRAG;              // E, beta, last: f32 [3][C]
+    static constexpr int COEF = FRAG;              // E, beta, last, scale E: f32 [4][C]
     // fragment (mt, gp <= mt / 2) of a lower triangular operand
     static __host__ __device__ constexpr int lower(int mt, int gp) { return mt < 2 ? mt : 2 * mt - 2 + gp; }
     // fragment (mt, gp >= mt / 2) of an upper triangular one

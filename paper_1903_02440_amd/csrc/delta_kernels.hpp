@@ -2,8 +2,6 @@
 // the states from chunk to chunk (gfx950).
 #pragma once
 
-#include <type_traits>
-
 #include "delta_chunk.hpp"
 
 namespace spk {
@@ -211,6 +209,7 @@ __global__ __launch_bounds__(PREP_THREADS) void k_delta_prep(const E *__restrict
                 co[tid] = expf((float)s);
                 co[C + tid] = be;
                 co[2 * C + tid] = expf((float)(end - s));
+                co[3 * C + tid] = a.scale * expf((float)s);
             }
         }
         __syncthreads();
@@ -227,7 +226,7 @@ __global__ __launch_bounds__(PREP_THREADS) void k_delta_prep(const E *__restrict
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int c = 32 * gp + slot(gr, j), lo = BWD ? i : c, hi = BWD ? c : i;
-                x[j] = lo <= hi ? expf((float)(gam[hi] - gam[lo])) * H[hi * PITCH + lo] : 0.0f;
+                x[j] = lo <= hi ? a.scale * expf((float)(gam[hi] - gam[lo])) * H[hi * PITCH + lo] : 0.0f;
             }
             put_frag<F::NP>(head + F::PAT + f * F::NP * FRAG, lane, split<F::NP>(x));
         }
@@ -341,15 +340,29 @@ __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Arg
         to_lds(dst, key + (int64_t)c * F::KEY, F::SCAN_KEY, wv, waves, lane);
         to_lds(dst + F::SCAN_KEY, head + (int64_t)c * F::HEAD, F::SCAN_HEAD, wv, waves, lane);
     };
+    // sample i of the chunk, column col: uniform rows and the lane's offset within four of them
     const int64_t vstep = (int64_t)a.Hv * a.dv;
-    const int64_t v0 = ((int64_t)b * a.L * a.Hv + h) * a.dv + col;
-    const E *vcol = v + ((int64_t)b * a.L * a.Hv + h) * a.dv + min(col, a.dv - 1);
+    const E *vrow = v + ((int64_t)b * a.L * a.Hv + h) * a.dv;
+    E *orow = out + ((int64_t)b * a.L * a.Hv + h) * a.dv;
+    const uint32_t lin = (uint32_t)((4 * gr * vstep + min(col, a.dv - 1)) * sizeof(E)),
+                   lout = (uint32_t)((4 * gr * vstep + col) * sizeof(E));
     E vv[MT][4];
-    auto values = [&](int c) {  // (clamped, not skipped: loads behind a branch would each be waited for)
+    auto values = [&](int c) {
+        const E *p = vrow + (int64_t)c * C * vstep;
+        if ((c + 1) * C <= n) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+            for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) vv[mt][r] = vcol[min(c * C + 16 * mt + 4 * gr + r, n - 1) * vstep];
+                for (int r = 0; r < 4; ++r) vv[mt][r] = at(p + (16 * mt + r) * vstep, lin);
+        } else {
+            // clamped, not skipped: loads behind a branch would each be waited for.  (Rows
+            // behind the last sample have beta = 0.)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    vv[mt][r] = p[min(16 * mt + 4 * gr + r, n - 1 - c * C) * vstep + min(col, a.dv - 1)];
+        }
     };
     if (nc) {
         values(0);
@@ -362,8 +375,10 @@ __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Arg
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                vc[mt][r] = live && c * C + 16 * mt + 4 * gr + r < n ? to_float(vv[mt][r]) : 0.0f;
+            for (int r = 0; r < 4; ++r) {
+                vc[mt][r] = to_float(vv[mt][r]);
+                if (STATES) vc[mt][r] = live ? vc[mt][r] : 0.0f;  // (the padding is read by others)
+            }
         if (c + 1 < nc) {
             values(c + 1);
             if (NBUF == 2) fetch(c + 1);
@@ -374,11 +389,12 @@ __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Arg
                        *P = T + F::PAT;
             const float *co = reinterpret_cast<const float *>(T + F::T);
             if (STATES) {
-                float *dst = kept.S + ((int64_t)bh * w.NC + c) * 32 * DS * kept.dvp + col;
+                float *dst = kept.S + ((int64_t)bh * w.NC + c) * 32 * DS * kept.dvp;
+                const uint32_t lo = (uint32_t)(4 * gr * kept.dvp + col) * 4;
 #pragma unroll
                 for (int t = 0; t < 2 * DS; ++t)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) dst[(int64_t)(16 * t + 4 * gr + r) * kept.dvp] = S[t][r];
+                    for (int r = 0; r < 4; ++r) at(dst + (16 * t + r) * kept.dvp, lo) = S[t][r];
             }
             f32x4 X[MT];
 #pragma unroll
@@ -396,14 +412,12 @@ __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Arg
                 }
             }
             f32x4 U[MT];
-            float e[MT][4];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
                 const f32x4 ev = *reinterpret_cast<const f32x4 *>(co + 16 * mt + 4 * gr);
                 const f32x4 be = *reinterpret_cast<const f32x4 *>(co + C + 16 * mt + 4 * gr);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    e[mt][r] = ev[r];
                     X[mt][r] = be[r] * (vc[mt][r] - ev[r] * X[mt][r]);
                 }
                 U[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -416,8 +430,7 @@ __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Arg
             }
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) Y[mt][r] *= STATES ? 1.0f : e[mt][r];
+                if (!STATES) Y[mt] *= *reinterpret_cast<const f32x4 *>(co + 3 * C + 16 * mt + 4 * gr);
             if (STATES) {
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) Y[mt] = U[mt];
@@ -447,15 +460,28 @@ __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Arg
         if (NBUF == 2) wait_copies();
         __syncthreads();
         if (NBUF == 1 && c + 1 < nc) fetch(c + 1);
-        if (mine) {
+        if (STATES && mine) {
+            float *dst = kept.U + ((int64_t)bh * w.NC + c) * C * kept.dvp;
+            const uint32_t lo = (uint32_t)(4 * gr * kept.dvp + col) * 4;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int i = c * C + 16 * mt + 4 * gr + r;
-                    if (STATES) kept.U[((int64_t)bh * w.NC * C + i) * kept.dvp + col] = Y[mt][r];
-                    else if (live && i < n) out[v0 + i * vstep] = from_float<E>(a.scale * Y[mt][r]);
-                }
+                for (int r = 0; r < 4; ++r) at(dst + (16 * mt + r) * kept.dvp, lo) = Y[mt][r];
+        }
+        if (!STATES && live) {
+            E *p = orow + (int64_t)c * C * vstep;
+            if ((c + 1) * C <= n) {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) at(p + (16 * mt + r) * vstep, lout) = from_float<E>(Y[mt][r]);
+            } else {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (c * C + 16 * mt + 4 * gr + r < n) at(p + (16 * mt + r) * vstep, lout) = from_float<E>(Y[mt][r]);
+            }
         }
         if (NBUF == 1) {
             wait_copies();
