@@ -24,61 +24,61 @@
 namespace spk {
 namespace delta {
 
-template <class E, int DS>
+// LDS of the reverse pass: K is needed all through a chunk and has two buffers
+// where they fit; Q and the coefficients, T^T and P^T from the middle on.
+template <class E, int DS, int KS>
 struct RscanLds {
     using F = Blob<E, DS, true>;
-    static constexpr int HEADP = F::HEAD - F::T;  // coefficients, T^T, P^T
-    static constexpr int EARLY = F::K + HEADP, LATE = 2 * F::KT;
-    static constexpr int NBUF = 2 * EARLY + LATE <= LDS_BYTES ? 2 : 1, BYTES = NBUF * EARLY + LATE;
+    static constexpr int TP = F::HEAD - F::T;  // coefficients, T^T, P^T
+    static constexpr int X = KS > 1 ? 8 * F::MT * FRAG : 0;
+    static constexpr int KB = 3 * F::K + TP + X <= LDS_BYTES ? 2 : 1;
+    static constexpr int AT_Q = KB * F::K, AT_TP = AT_Q + F::K, AT_X = AT_TP + TP, BYTES = AT_X + X;
+    static_assert(BYTES <= LDS_BYTES, "LDS");
 };
 
-// Grid and columns as the states' kernel (delta_kernels.hpp), chunks from last
-// to first; a wave carries 16 columns of dS.  K, T^T, P^T and the coefficients
-// are needed from the start of a chunk, K^T and Q^T in its second half only: with
-// NBUF = 2 the former have two buffers and come during the chunk before, the
-// latter one and come during the first half (what fits the LDS).
-template <class E, int DS, int NBUF>
+// Grid, columns and parts as the states' kernel (delta_kernels.hpp), chunks from
+// last to first; the waves of a tile carry 16 columns of dS and add up K dS
+// through LDS.
+template <class E, int DS, int KS>
 __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out, Args a,
-                                                     const int32_t *__restrict__ lengths, int compute, Chunks w,
+                                                     const int32_t *__restrict__ lengths, int tiles, Chunks w,
                                                      Kept kept, const float *d_last, float *d_first) {
     using F = Blob<E, DS, true>;
-    constexpr int C = F::C, MT = F::MT, NT = F::NT, GP = F::GP;
-    using R = RscanLds<E, DS>;
+    using M = RscanLds<E, DS, KS>;
+    constexpr int C = F::C, MT = F::MT, NT = F::NT, GP = F::GP, DW = DS / KS;
     extern __shared__ char lds[];
     const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, gr = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+    const int tile = wv / KS, part = wv % KS, s0 = part * DW;
     const int bh = head_of(blockIdx.x, gridDim.x), b = bh / a.Hv, h = bh % a.Hv, hk = h / (a.Hv / a.Hk);
     const int n = lengths ? max(0, min(a.L, lengths[b])) : a.L, nc = (n + C - 1) / C;
-    const int col = ((int)blockIdx.y * compute + wv) * 16 + m;
-    const bool mine = wv < compute && col - m < kept.dvp, live = mine && col < a.dv;
-    const int64_t s0 = (int64_t)bh * a.dk * a.dv + col;
+    const int col = ((int)blockIdx.y * tiles + tile) * 16 + m;
+    const bool mine = tile < tiles && col - m < kept.dvp, live = mine && col < a.dv;
     const char *key = w.key + ((int64_t)b * a.Hk + hk) * w.NC * F::KEY;
     const char *head = w.head + (int64_t)bh * w.NC * F::HEAD + F::T;
-    f32x4 S[2 * DS];
+    f32x4 S[2 * DW];
 #pragma unroll
-    for (int t = 0; t < 2 * DS; ++t) S[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < 2 * DW; ++t) S[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
     if (d_last) {
         const float *from = d_last + (int64_t)bh * a.dk * a.dv + min(col, a.dv - 1);
 #pragma unroll
-        for (int t = 0; t < 2 * DS; ++t)
+        for (int t = 0; t < 2 * DW; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) S[t][r] = from[(int64_t)min(16 * t + 4 * gr + r, a.dk - 1) * a.dv];
+            for (int r = 0; r < 4; ++r) S[t][r] = from[(int64_t)min(dk_of(2 * s0 + t, 4 * gr + r), a.dk - 1) * a.dv];
 #pragma unroll
-        for (int t = 0; t < 2 * DS; ++t)
+        for (int t = 0; t < 2 * DW; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) S[t][r] = live && 16 * t + 4 * gr + r < a.dk ? S[t][r] : 0.0f;
+            for (int r = 0; r < 4; ++r) S[t][r] = live && dk_of(2 * s0 + t, 4 * gr + r) < a.dk ? S[t][r] : 0.0f;
     }
-    char *late = lds + NBUF * R::EARLY;
-    auto fetch_early = [&](int c) {
-        char *dst = lds + (c % NBUF) * R::EARLY;
-        to_lds(dst, key + (int64_t)c * F::KEY, F::K, wv, waves, lane);
-        to_lds(dst + F::K, head + (int64_t)c * F::HEAD, R::HEADP, wv, waves, lane);
+    auto fetch_k = [&](int c) { to_lds(lds + (c % M::KB) * F::K, key + (int64_t)c * F::KEY, F::K, wv, waves, lane); };
+    auto fetch_rest = [&](int c) {
+        to_lds(lds + M::AT_TP, head + (int64_t)c * F::HEAD, M::TP, wv, waves, lane);
+        to_lds(lds + M::AT_Q, key + (int64_t)c * F::KEY + F::K, F::K, wv, waves, lane);
     };
-    auto fetch_late = [&](int c) { to_lds(late, key + (int64_t)c * F::KEY + F::K, R::LATE, wv, waves, lane); };
     const int64_t vstep = (int64_t)a.Hv * a.dv;
     const E *orow = d_out + ((int64_t)b * a.L * a.Hv + h) * a.dv;
     const uint32_t lin = (uint32_t)((4 * gr * vstep + min(col, a.dv - 1)) * sizeof(E)),
-                   lkept = (uint32_t)(4 * gr * kept.dvp + col) * 4;
+                   lkept = (uint32_t)(4 * gr * kept.dvp + col) * 4, lstate = (uint32_t)(8 * gr * kept.dvp + col) * 4;
     E on[MT][4];
     auto upstream = [&](int c) {
         const E *p = orow + (int64_t)c * C * vstep;
@@ -97,39 +97,66 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
     };
     if (nc) {
         upstream(nc - 1);
-        fetch_early(nc - 1);
-        if (NBUF == 1) fetch_late(nc - 1);
+        fetch_k(nc - 1);
         wait_copies();
+        fetch_rest(nc - 1);
     }
     __syncthreads();
     for (int c = nc - 1; c >= 0; --c) {
+        const char *K = lds + (c % M::KB) * F::K, *Q = lds + M::AT_Q, *H = lds + M::AT_TP;
+        const char *TT = H + (F::TTAT - F::T), *PT = H + (F::PAT - F::T);
+        const float *co = reinterpret_cast<const float *>(H);
+        f32x4 X[MT], Y[MT];
+        if (mine) {
+            float *dst = kept.dS + ((int64_t)bh * w.NC + c) * 32 * DS * kept.dvp;
+#pragma unroll
+            for (int t = 0; t < 2 * DW; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    at(dst + (32 * (s0 + (t >> 1)) + 4 * (t & 1) + r) * kept.dvp, lstate) = S[t][r];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) X[mt] = Y[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < DW; ++s) {
+                const Terms<3> st = split<3>(S[2 * s], S[2 * s + 1]);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) mma<NT, 3>(X[mt], frag<NT>(K + (mt * DS + s0 + s) * NT * FRAG, lane), st);
+            }
+            if (KS > 1) {
+                char *xb = lds + M::AT_X + tile * KS * MT * FRAG;
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+                    *reinterpret_cast<f32x4 *>(xb + (part * MT + mt) * FRAG + lane * 16) = X[mt];
+            }
+        }
+        wait_copies();  // what the second half needs of this chunk
+        lds_barrier();
         float o[MT][4];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
                 o[mt][r] = live && c * C + 16 * mt + 4 * gr + r < n ? to_float(on[mt][r]) : 0.0f;
-        if (c > 0) upstream(c - 1);
-        if (NBUF == 2) fetch_late(c);
-        const char *K = lds + (c % NBUF) * R::EARLY, *H = K + F::K, *KT = late, *QT = late + F::KT;
-        const char *TT = H + (F::TTAT - F::T), *PT = H + (F::PAT - F::T);
-        const float *co = reinterpret_cast<const float *>(H);
-        f32x4 Y[MT];
+        if (c > 0) {
+            upstream(c - 1);
+            if (M::KB == 2) fetch_k(c - 1);
+        }
         if (mine) {
-            float *dst = kept.dS + ((int64_t)bh * w.NC + c) * 32 * DS * kept.dvp;
+            if (KS > 1) {
+                const char *xb = lds + M::AT_X + tile * KS * MT * FRAG;
 #pragma unroll
-            for (int t = 0; t < 2 * DS; ++t)
+                for (int mt = 0; mt < MT; ++mt) {
+                    f32x4 x[KS];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) at(dst + (16 * t + r) * kept.dvp, lkept) = S[t][r];
-            f32x4 X[MT], Z[MT];
+                    for (int p = 0; p < KS; ++p) x[p] = *reinterpret_cast<const f32x4 *>(xb + (p * MT + mt) * FRAG + lane * 16);
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) X[mt] = Z[mt] = Y[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int s = 0; s < DS; ++s) {
-                const Terms<3> st = split<3>(S[2 * s], S[2 * s + 1]);
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) mma<NT, 3>(X[mt], frag<NT>(K + (mt * DS + s) * NT * FRAG, lane), st);
+                    for (int p = 1; p < KS; ++p) x[0] += x[p];
+                    X[mt] = x[0];
+                }
             }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)  // dU: last (K dS), and P^T dO on top
+                X[mt] *= *reinterpret_cast<const f32x4 *>(co + 2 * C + 16 * mt + 4 * gr);
 #pragma unroll
             for (int gp = 0; gp < GP; ++gp) {
                 float x[8];
@@ -137,12 +164,7 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
                 for (int j = 0; j < 8; ++j) x[j] = o[2 * gp + (j >> 2)][j & 3];
                 const Terms<NT> ot = split<NT>(x);
 #pragma unroll
-                for (int mt = 0; mt <= 2 * gp + 1; ++mt) mma<3, NT>(Z[mt], frag<3>(PT + F::upper(mt, gp) * 3 * FRAG, lane), ot);
-            }
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                const f32x4 la = *reinterpret_cast<const f32x4 *>(co + 2 * C + 16 * mt + 4 * gr);
-                X[mt] = la * X[mt] + Z[mt];  // dU
+                for (int mt = 0; mt <= 2 * gp + 1; ++mt) mma<3, NT>(X[mt], frag<3>(PT + F::upper(mt, gp) * 3 * FRAG, lane), ot);
             }
 #pragma unroll
             for (int gp = 0; gp < GP; ++gp) {
@@ -150,23 +172,9 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
 #pragma unroll
                 for (int mt = 0; mt <= 2 * gp + 1; ++mt) mma<3, 3>(Y[mt], frag<3>(TT + F::upper(mt, gp) * 3 * FRAG, lane), ut);
             }
-        }
-        if (NBUF == 2) {
-            wait_copies();
-            __syncthreads();
-            if (c > 0) fetch_early(c - 1);
-        }
-        if (mine) {
-            float *yd = kept.Y + ((int64_t)bh * w.NC + c) * C * kept.dvp;
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) at(yd + (16 * mt + r) * kept.dvp, lkept) = Y[mt][r];
             const float end = co[C - 1];
 #pragma unroll
-            for (int t = 0; t < 2 * DS; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) S[t][r] *= end;
+            for (int t = 0; t < 2 * DW; ++t) S[t] *= end;
 #pragma unroll
             for (int gp = 0; gp < GP; ++gp) {
                 float x[8], y[8];
@@ -183,29 +191,37 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
                 }
                 const Terms<3> xt = split<3>(x), yt = split<3>(y);
 #pragma unroll
-                for (int t = 0; t < 2 * DS; ++t) {
-                    mma<NT, 3>(S[t], frag<NT>(QT + (t * GP + gp) * NT * FRAG, lane), xt);
-                    mma<NT, 3>(S[t], frag<NT>(KT + (t * GP + gp) * NT * FRAG, lane), yt);
+                for (int t = 0; t < 2 * DW; ++t) {
+                    mma<NT, 3>(S[t], tfrag<NT, DS>(Q, 2 * s0 + t, gp, lane), xt);
+                    mma<NT, 3>(S[t], tfrag<NT, DS>(K, 2 * s0 + t, gp, lane), yt);
                 }
             }
         }
-        if (NBUF == 1) {
-            __syncthreads();
-            if (c > 0) {
-                fetch_early(c - 1);
-                fetch_late(c - 1);
+        wait_copies();
+        lds_barrier();
+        if (c > 0 && M::KB == 1) fetch_k(c - 1);
+        if (M::KB == 1) {
+            wait_copies();
+            lds_barrier();
+        }
+        if (c > 0) fetch_rest(c - 1);
+        if (mine) {
+            float *yd = kept.Y + ((int64_t)bh * w.NC + c) * C * kept.dvp;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                if (part != mt * KS / MT) continue;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) at(yd + (16 * mt + r) * kept.dvp, lkept) = Y[mt][r];
             }
         }
-        wait_copies();
-        __syncthreads();
     }
     if (!live || !d_first) return;
 #pragma unroll
-    for (int t = 0; t < 2 * DS; ++t)
+    for (int t = 0; t < 2 * DW; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int d = 16 * t + 4 * gr + r;
-            if (d < a.dk) d_first[s0 + (int64_t)d * a.dv] = S[t][r];
+            const int d = dk_of(2 * s0 + t, 4 * gr + r);
+            if (d < a.dk) d_first[(int64_t)bh * a.dk * a.dv + (int64_t)d * a.dv + col] = S[t][r];
         }
 }
 
@@ -218,8 +234,12 @@ struct GradLds {
     static constexpr int ONE = B::MT * (B::NT + 6) * FRAG;  // dO, Y, U of 32 columns
     static constexpr int TRI = B::TRI * 3 * FRAG;           // N, M, N^T, (beta M)^T: four of these
     static constexpr int SUMS = (2 * GRAD_WAVES + 2) * B::C * 4 + GRAD_WAVES * 4;
-    // the staged columns and M, N as floats are done with before the four triangles are read
-    static constexpr int AT_SQ = ONE, AT_TRI = ONE + 2 * SQ, AT_SUMS = AT_TRI + 4 * TRI;
+    // K and Q take the room of the staged columns and of M and N as floats, once the
+    // four triangles are made, where they do not fit beside them
+    static constexpr int KQ = 2 * B::K, TEMP = ONE + 2 * SQ;
+    static constexpr bool APART = KQ + TEMP + 4 * TRI + SUMS + 8 * 1024 <= LDS_BYTES;
+    static constexpr int AT_KQ = APART ? TEMP : 0, R0 = APART ? TEMP + KQ : (KQ > TEMP ? KQ : TEMP);
+    static constexpr int AT_SQ = ONE, AT_TRI = R0, AT_SUMS = AT_TRI + 4 * TRI;
     static constexpr int AT_GAM = AT_SUMS + (SUMS + 15) / 16 * 16, BYTES = AT_GAM + B::C * 8 + 4 * B::C * 4;
 };
 
@@ -253,6 +273,9 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
     float *co = reinterpret_cast<float *>(gam + C);  // E, beta, last
     const char *key = w.key + ((int64_t)blockIdx.y * w.NC + chunk) * F::KEY;
     const int64_t row0 = (int64_t)b * a.L + chunk * C;
+
+    const char *fk = lds + G::AT_KQ, *fq = fk + F::K;
+    if (G::APART) to_lds(lds + G::AT_KQ, key, G::KQ, wv, GRAD_WAVES, lane);
 
     f32x4 dqs[TW][MT], dks[TW][MT];
 #pragma unroll
@@ -326,8 +349,8 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
             for (int p = 0; p < TW; ++p) {
                 const int t = p * GRAD_WAVES + wv;
                 if (t >= 2 * DS) continue;
-                const float *ps = S + (int64_t)(16 * t + m) * kept.dvp + 32 * vg + 4 * gr;
-                const float *pd = dS + (int64_t)(16 * t + m) * kept.dvp + 32 * vg + 4 * gr;
+                const float *ps = S + (int64_t)dk_of(t, m) * kept.dvp + 32 * vg + 4 * gr;
+                const float *pd = dS + (int64_t)dk_of(t, m) * kept.dvp + 32 * vg + 4 * gr;
                 const f32x4 s0 = *reinterpret_cast<const f32x4 *>(ps), s1 = *reinterpret_cast<const f32x4 *>(ps + 16);
                 const f32x4 e0 = *reinterpret_cast<const f32x4 *>(pd), e1 = *reinterpret_cast<const f32x4 *>(pd + 16);
 #pragma unroll
@@ -389,6 +412,11 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
             put_frag<3>(tri + which * G::TRI + f * 3 * FRAG, lane, split<3>(x));
         }
         __syncthreads();
+        if (!G::APART) to_lds(lds + G::AT_KQ, key, G::KQ, wv, GRAD_WAVES, lane);
+        if (!G::APART || hr == 0) {
+            wait_copies();
+            lds_barrier();
+        }
         float pg[MT][4], pb[MT][4], pe = 0.0f;  // row sums: dgamma, k.r; k.(last U dS^T) of all rows
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
@@ -396,7 +424,7 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
             for (int r = 0; r < 4; ++r) pg[mt][r] = pb[mt][r] = 0.0f;
 #pragma unroll
         for (int p = 0; p < TW; ++p) {
-            const int t = p * GRAD_WAVES + wv, d = 16 * t + m;
+            const int t = p * GRAD_WAVES + wv, d = dk_of(t, m);
             if (t >= 2 * DS) continue;
             E ke[MT][4], qe[MT][4];
 #pragma unroll
@@ -410,8 +438,8 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
             Terms<NT> kt[GP], qt[GP];
 #pragma unroll
             for (int gp = 0; gp < GP; ++gp) {
-                kt[gp] = frag<NT>(key + F::K + (t * GP + gp) * NT * FRAG, lane);
-                qt[gp] = frag<NT>(key + F::K + F::KT + (t * GP + gp) * NT * FRAG, lane);
+                kt[gp] = tfrag<NT, DS>(fk, t, gp, lane);
+                qt[gp] = tfrag<NT, DS>(fq, t, gp, lane);
             }
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
@@ -492,7 +520,7 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
     }
 #pragma unroll
     for (int p = 0; p < TW; ++p) {
-        const int t = p * GRAD_WAVES + wv, d = 16 * t + m;
+        const int t = p * GRAD_WAVES + wv, d = dk_of(t, m);
         if (t >= 2 * DS || d >= a.dk) continue;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
@@ -525,6 +553,14 @@ size_t carve(void *ws, const Args &a, Chunks *w, Kept *kept) {
     return spk::align_up(c.off, 256);
 }
 
+template <class E, int DS, int KS>
+void launch_rscan(const Cols &cols, const E *d_out, const Args &a, const int32_t *lengths, const Chunks &w,
+                  const Kept &kept, const float *d_last, float *d_first, hipStream_t st) {
+    constexpr int LDS = RscanLds<E, DS, KS>::BYTES;
+    hipLaunchKernelGGL((k_delta_rscan<E, DS, KS>), dim3((unsigned)(a.B * a.Hv), (unsigned)cols.blocks),
+                       dim3((unsigned)cols.threads), LDS, st, d_out, a, lengths, cols.tiles, w, kept, d_last, d_first);
+}
+
 struct Call {
     const void *q, *k, *v;
     const float *g, *beta;
@@ -538,7 +574,6 @@ struct Call {
 
 template <class E, int DS>
 int backward(const Call &c, const Args &a, void *ws, hipStream_t st, const char *name) {
-    using F = Blob<E, DS, true>;
     constexpr int LP = PrepLds<E, DS>::BYTES, LG = GradLds<E, DS>::BYTES;
     Chunks w;
     Kept kept;
@@ -547,17 +582,13 @@ int backward(const Call &c, const Args &a, void *ws, hipStream_t st, const char 
     const E *d_out = static_cast<const E *>(c.d_out);
     const dim3 per_key((unsigned)w.NC, (unsigned)(a.B * a.Hk));
     hipLaunchKernelGGL((k_delta_prep<E, DS, true>), per_key, dim3(PREP_THREADS), LP, st, q, k, c.g, c.beta, a, c.lengths, wide_rows<E>(a.dk, q, k), w);
-    const int tiles = kept.dvp / 16, compute = scan_waves(a, tiles);
-    const dim3 cols((unsigned)(a.B * a.Hv), (unsigned)((tiles + compute - 1) / compute));
-    const dim3 threads(64 * std::max(4, compute));
-    constexpr int NB = 2 * F::SCAN <= LDS_BYTES ? 2 : 1;
-    hipLaunchKernelGGL((k_delta_scan<E, DS, NB, true>), cols, threads, NB * F::SCAN, st, v, a, c.lengths, compute, w,
-                       c.state_in, (E *)nullptr, (float *)nullptr, kept);
-    using R = RscanLds<E, DS>;
-    constexpr int LR = R::BYTES, NR = R::NBUF;
-    static_assert(LR <= LDS_BYTES && F::SCAN <= LDS_BYTES && LP <= LDS_BYTES && LG <= LDS_BYTES, "LDS");
-    hipLaunchKernelGGL((k_delta_rscan<E, DS, NR>), cols, threads, LR, st, d_out, a, c.lengths, compute, w, kept,
-                       c.d_last, c.d_first);
+    static_assert(LP <= LDS_BYTES && LG <= LDS_BYTES, "LDS");
+    const Cols cols = columns(a, kept.dvp / 16, DS);
+#define SPK_SCAN(KS)                                                                                                \
+    launch_scan<E, DS, KS, true>(cols, v, a, c.lengths, w, c.state_in, nullptr, nullptr, kept, st);                 \
+    launch_rscan<E, DS, KS>(cols, d_out, a, c.lengths, w, kept, c.d_last, c.d_first, st)
+    SPK_DELTA_PARTS(DS, cols, SPK_SCAN)
+#undef SPK_SCAN
     hipLaunchKernelGGL((k_delta_grads<E, DS>), per_key, dim3(GRAD_THREADS), LG, st, q, k, v, c.g, d_out, a, c.lengths, w, kept, static_cast<E *>(c.d_q), static_cast<E *>(c.d_k),
                        static_cast<E *>(c.d_v), c.d_g, c.d_beta);
     return spk::check_launch(name);

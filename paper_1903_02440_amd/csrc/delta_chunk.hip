@@ -1,8 +1,6 @@
 // The gated delta rule over chunks of samples (gfx950): the batch call.  The
 // formulas and the operands' layout are in delta_chunk.hpp, the kernels that it
 // shares with the backward pass in delta_kernels.hpp.
-#include <algorithm>
-
 #include "delta_kernels.hpp"
 
 namespace spk {
@@ -22,21 +20,18 @@ template <class E, int DS>
 int forward(const void *q, const void *k, const void *v, const float *g, const float *beta, const Args &a,
             const int32_t *lengths, const float *state_in, void *out, float *state_out, void *ws, hipStream_t st,
             const char *name) {
-    using F = Blob<E, DS, false>;
     Chunks w;
     carve<E, DS>(ws, a, &w);
-    const E *qe = static_cast<const E *>(q), *ke = static_cast<const E *>(k), *ve = static_cast<const E *>(v);
+    const E *qe = static_cast<const E *>(q), *ke = static_cast<const E *>(k);
     const int wide = wide_rows<E>(a.dk, q, k);
     constexpr int LP = PrepLds<E, DS>::BYTES;
+    static_assert(LP <= LDS_BYTES, "LDS");
     hipLaunchKernelGGL((k_delta_prep<E, DS, false>), dim3((unsigned)w.NC, (unsigned)(a.B * a.Hk)), dim3(PREP_THREADS), LP, st,
                        qe, ke, g, beta, a, lengths, wide, w);
-    constexpr int ONE = F::SCAN, NBUF = 2 * ONE <= LDS_BYTES ? 2 : 1;
-    static_assert(ONE <= LDS_BYTES && LP <= LDS_BYTES, "LDS");
-    const int tiles = (a.dv + 15) / 16, compute = scan_waves(a, tiles), waves = std::max(4, compute);
-    hipLaunchKernelGGL((k_delta_scan<E, DS, NBUF, false>),
-                       dim3((unsigned)(a.B * a.Hv), (unsigned)((tiles + compute - 1) / compute)), dim3(64 * waves),
-                       NBUF * ONE, st, ve, a, lengths, compute, w, state_in, static_cast<E *>(out), state_out,
-                       Kept{});
+    const Cols cols = columns(a, (a.dv + 15) / 16, DS);
+#define SPK_SCAN(KS) launch_scan<E, DS, KS, false>(cols, v, a, lengths, w, state_in, out, state_out, Kept{}, st)
+    SPK_DELTA_PARTS(DS, cols, SPK_SCAN)
+#undef SPK_SCAN
     return spk::check_launch(name);
 }
 

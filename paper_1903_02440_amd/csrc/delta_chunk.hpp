@@ -18,10 +18,12 @@
 //
 // Operands lie in fragments: for 16 rows and 32 summed indices the 16 bytes of
 // each lane in turn (1 KiB a term).  The result of a matrix instruction holds,
-// in lane (n, g), rows 4g..4g+3 of column n; taking two result tiles as one
-// right operand gives lane group g the indices 4g..4g+3 and 16+4g..16+4g+3 of
-// the 32.  Fragments are laid out for that order, so results feed the next
-// product without leaving their lane.
+// in lane (n, g), rows 4g..4g+3 of column n; two result tiles taken as one right
+// operand give lane group g eight of the 32 indices.  The left operands are laid
+// out for that order, so results feed the next product without leaving their
+// lane: samples go by slot() below, and the rows of the state's tiles are dealt
+// out by dk_of() so that lane group g holds 8g..8g+7, as a row of K lies in
+// memory.  K^T is read from the fragments of K by the LDS's transposing reads.
 #pragma once
 
 #include <type_traits>
@@ -37,8 +39,11 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int FRAG = 1024;  // bytes of one term of a fragment
 
-// index within a group of 32 of element j of lane group g
+// index within a group of 32 samples (or columns) of element j of lane group g
 __device__ __forceinline__ int slot(int g, int j) { return j < 4 ? 4 * g + j : 12 + 4 * g + j; }
+
+// index in dk of row i of the state's tile t
+__device__ __forceinline__ int dk_of(int t, int i) { return 32 * (t >> 1) + 8 * (i >> 2) + 4 * (t & 1) + (i & 3); }
 
 template <int N>
 struct Terms {
@@ -122,6 +127,29 @@ __device__ __forceinline__ void put_frag(char *p, int lane, const Terms<N> &x) {
     for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4 *>(p + i * FRAG + lane * 16) = x.t[i];
 }
 
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// Fragment of the transpose of K (or Q) in LDS: rows of the state's tile t,
+// samples of group gp.  A transposing read gives lane i of a group of 16 the
+// i-th column of four rows of 16, here four samples' values of dk_of(t, i).
+template <int NT, int DS>
+__device__ __forceinline__ Terms<NT> tfrag(const char *k, int t, int gp, int lane) {
+    const int i = lane & 15, g = lane >> 4;
+    Terms<NT> r;
+#pragma unroll
+    for (int x = 0; x < NT; ++x)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+            const char *p = k + (((2 * gp + hf) * DS + (t >> 1)) * NT + x) * FRAG + ((i & 3) * 16 + 4 * g + (i >> 2)) * 16 +
+                            8 * (t & 1);
+            const s16x4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) s16x4 *)const_cast<char *>(p));
+            const uint2 u = __builtin_bit_cast(uint2, w);
+            r.t[x][2 * hf] = u.x, r.t[x][2 * hf + 1] = u.y;
+        }
+    return r;
+}
+
 // Sizes of a chunk's operands.  DS: groups of 32 of dk; MT: tiles of 16
 // samples.  Float inputs take chunks of 32 samples, so that their three terms
 // fit the LDS at dk = 256; bfloat16 ones take 64.
@@ -143,7 +171,6 @@ struct Lay {
     // a triangular C x C operand: the fragments that are not zero throughout
     static constexpr int TRI = MT == 4 ? 6 : 2;
     static constexpr int K = MT * DS * NT * FRAG;  // rows of K (or Q), summed over dk: [mt][s][term]
-    static constexpr int KT = 2 * DS * GP * NT * FRAG;  // its transpose, summed over the samples: [t][gp][term]
     static constexpr int COEF = FRAG;              // E, beta, last, scale E: f32 [4][C]
     // fragment (mt, gp <= mt / 2) of a lower triangular operand
     static __host__ __device__ constexpr int lower(int mt, int gp) { return mt < 2 ? mt : 2 * mt - 2 + gp; }
@@ -173,6 +200,8 @@ __device__ __forceinline__ void to_lds(char *dst, const char *src, int n, int wa
 }
 // All of the wave's copies and loads have arrived, its stores are out.  (As a
 // builtin the compiler counts it too: loads before it need no wait of their own.)
+// A barrier that hands LDS over; copies and loads may stay in flight.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ __forceinline__ void wait_copies() {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)

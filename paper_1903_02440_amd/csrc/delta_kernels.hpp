@@ -10,20 +10,17 @@ namespace delta {
 constexpr int LDS_BYTES = 160 * 1024;
 
 // What the operand kernel leaves for the others, per (sequence, key head, chunk)
-// and per (sequence, value head, chunk), in bytes:
-//   forward   K, K^T, Q        T, coefficients, P
-//   backward  K, K^T, Q^T      T, coefficients, T^T, P^T
-// The states' kernel reads SCAN_KEY and SCAN_HEAD bytes of each from the start.
+// the fragments of K and Q, and per (sequence, value head, chunk), in bytes:
+//   forward   T, coefficients, P
+//   backward  T, coefficients, T^T, P^T
 template <class E, int DS, bool BWD>
 struct Blob : Lay<E, DS> {
     using B = Lay<E, DS>;
     static constexpr int NP = BWD ? 3 : B::NP;
-    static constexpr int KEY = BWD ? B::K + 2 * B::KT : 2 * B::K + B::KT;
+    static constexpr int KEY = 2 * B::K;
     static constexpr int T = B::TRI * 3 * FRAG, P = B::TRI * NP * FRAG;
     static constexpr int TTAT = T + B::COEF, PAT = TTAT + (BWD ? T : 0);
     static constexpr int HEAD = PAT + P;
-    static constexpr int SCAN_KEY = BWD ? B::K + B::KT : KEY, SCAN_HEAD = BWD ? T + B::COEF : HEAD;
-    static constexpr int SCAN = SCAN_KEY + SCAN_HEAD;
 };
 
 struct Chunks {
@@ -40,9 +37,9 @@ struct Kept {
     float *S, *dS, *U, *Y;
 };
 
-// Eight elements of a row of keys or queries, as two runs of four (32 s + 4 g on
-// and 16 later), in the row's own type.  Indices past the row are clamped and the
-// elements set to 0 by the caller: loads behind a branch would each be waited for.
+// Eight elements of a row of keys or queries from 32 s + 8 g on, in the row's own
+// type.  Indices past the row are clamped and the elements set to 0 afterwards:
+// loads behind a branch would each be waited for.
 template <class E>
 struct Raw8 {
     E e[8];
@@ -50,27 +47,24 @@ struct Raw8 {
 template <class E, bool WIDE>
 __device__ __forceinline__ Raw8<E> load8(const E *p, int s, int g, int dk) {
     Raw8<E> r;
+    const int c = 32 * s + 8 * g;
+    if constexpr (WIDE) {  // dk a multiple of 8, rows on 16 bytes
+        struct alignas(16) Eight {
+            E e[8];
+        };
+        const Eight w = *reinterpret_cast<const Eight *>(p + min(c, dk - 8));
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int c = 32 * s + 4 * g + 16 * h;
-        if constexpr (WIDE) {  // dk a multiple of 4, rows aligned to four elements
-            struct alignas(4 * sizeof(E)) Four {
-                E e[4];
-            };
-            const Four w = *reinterpret_cast<const Four *>(p + min(c, dk - 4));
+        for (int j = 0; j < 8; ++j) r.e[j] = w.e[j];
+    } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) r.e[4 * h + j] = w.e[j];
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) r.e[4 * h + j] = p[min(c + j, dk - 1)];
-        }
+        for (int j = 0; j < 8; ++j) r.e[j] = p[min(c + j, dk - 1)];
     }
     return r;
 }
 template <class E>
 __device__ __forceinline__ void as_floats(const Raw8<E> &w, int s, int g, int dk, bool row, float (&x)[8]) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = row && 32 * s + slot(g, j) < dk ? to_float(w.e[j]) : 0.0f;
+    for (int j = 0; j < 8; ++j) x[j] = row && 32 * s + 8 * g + j < dk ? to_float(w.e[j]) : 0.0f;
 }
 
 constexpr int PREP_THREADS = 256;
@@ -112,7 +106,7 @@ __global__ __launch_bounds__(PREP_THREADS) void k_delta_prep(const E *__restrict
                                                              const int32_t *__restrict__ lengths, int wide, Chunks w) {
     using F = Blob<E, DS, BWD>;
     using S = PrepLds<E, DS>;
-    constexpr int C = F::C, MT = F::MT, NT = F::NT, GP = F::GP, PITCH = S::PITCH;
+    constexpr int C = F::C, MT = F::MT, NT = F::NT, PITCH = S::PITCH;
     extern __shared__ char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, m = lane & 15, gr = lane >> 4;
     const int chunk = blockIdx.x, b = blockIdx.y / a.Hk, hk = blockIdx.y % a.Hk, rep = a.Hv / a.Hk;
@@ -146,32 +140,13 @@ __global__ __launch_bounds__(PREP_THREADS) void k_delta_prep(const E *__restrict
                 const Terms<NT> t = split<NT>(y);
                 const int o = (mt * DS + s) * NT * FRAG;
                 put_frag<NT>((isq ? fq : fk) + o, lane, t);
-                if (!isq || !BWD) put_frag<NT>(key + (isq ? F::K + F::KT : 0) + o, lane, t);
+                put_frag<NT>(key + (isq ? F::K : 0) + o, lane, t);
             }
         }
     };
     if (wide) units(std::true_type{});
     else units(std::false_type{});
     __syncthreads();
-    // K^T (and Q^T): row d = 16 t + m, samples slot(gr, j) of group gp
-    constexpr int TF = 2 * DS * GP * NT;
-    for (int u = tid; u < (BWD ? 2 : 1) * TF * 64; u += PREP_THREADS) {
-        const bool isq = u >= TF * 64;
-        const int f = (u >> 6) - (isq ? TF : 0), term = f % NT, gp = f / NT % GP, t = f / (NT * GP);
-        const char *src = isq ? fq : fk;
-        const int d = 16 * t + m, s = d >> 5, r = d & 31, gd = (r & 15) >> 2, jd = (r >> 4) * 4 + (r & 3);
-        uint16_t e[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int i = 32 * gp + slot(gr, j);
-            e[j] = *reinterpret_cast<const uint16_t *>(src + (((i >> 4) * DS + s) * NT + term) * FRAG +
-                                                       (gd * 16 + (i & 15)) * 16 + jd * 2);
-        }
-        u32x4 o;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) o[j] = (uint32_t)e[2 * j] | ((uint32_t)e[2 * j + 1] << 16);
-        *reinterpret_cast<u32x4 *>(key + F::K + (isq ? F::KT : 0) + f * FRAG + lane * 16) = o;
-    }
     // lower tiles of K K^T (rows 0..MT-1 of the list) and Q K^T (the rest, from the last row on)
     for (int row = wv; row < 2 * MT; row += PREP_THREADS / 64) {
         const bool isq = row >= MT;
@@ -297,55 +272,79 @@ __global__ __launch_bounds__(PREP_THREADS) void k_delta_prep(const E *__restrict
 // key head, which read the same operands, on one XCD's L2.
 __device__ __forceinline__ int head_of(int x, int n) { return n % 8 == 0 ? (x & 7) * (n >> 3) + (x >> 3) : x; }
 
-// Grid (b * Hv + value head, block of columns): a wave carries 16 columns of the
-// state through the chunks, in registers: as the right operand of K S and Q S
-// (three terms) and as the sums of K^T (last U).  The waves of a workgroup share
-// the chunk's operands in LDS and wait for each other only there.  NBUF buffers:
-// with two, the next chunk's operands are on their way during this one's products.
-// STATES: for the backward pass, the state that enters each chunk and U are
-// written instead of out (`kept`).
-template <class E, int DS, int NBUF, bool STATES>
+// LDS of the states' kernel, for KS waves to a tile of 16 columns and at most
+// eight in all.  K is needed all through a chunk and has two buffers where they
+// fit; T, the coefficients and P from the middle on, with two where those still
+// fit; Q is done with in the middle and has one.  Then the partial sums that the
+// waves of a tile exchange.
+template <class E, int DS, int KS, bool STATES>
+struct ScanLds {
+    using F = Blob<E, DS, STATES>;
+    static constexpr int Q = STATES ? 0 : F::K, TP = STATES ? F::T + F::COEF : F::HEAD;
+    static constexpr int TILES = 8 / KS;
+    static constexpr int X = KS > 1 ? 8 * F::MT * FRAG : 0;
+    static constexpr int Y = STATES ? 0 : TILES * F::MT * (KS - 1) * FRAG;
+    static constexpr int KB = 2 * F::K + Q + TP + X + Y <= LDS_BYTES ? 2 : 1;
+    static constexpr int TB = KB * F::K + Q + 2 * TP + X + Y <= LDS_BYTES ? 2 : 1;
+    static constexpr int AT_Q = KB * F::K, AT_TP = AT_Q + Q, AT_X = AT_TP + TB * TP, AT_Y = AT_X + X,
+                         BYTES = AT_Y + Y;
+    static_assert(BYTES <= LDS_BYTES, "LDS");
+};
+
+// Grid (b * Hv + value head, block of columns): KS waves carry 16 columns of the
+// state through the chunks, each the rows of its DS / KS groups of 32 of dk, in
+// registers: as the right operand of K S and Q S (three terms) and as the sums of
+// K^T (last U).  They add up K S through LDS in the middle of a chunk, after
+// which each has U for itself; of out each finishes some rows.  KS = 1 where the
+// columns alone fill the SIMDs, more where they do not.  Waves without columns
+// help to copy.  STATES: for the backward pass, the state that enters each chunk
+// and U are written instead of out (`kept`).
+template <class E, int DS, int KS, bool STATES>
 __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Args a,
-                                                    const int32_t *__restrict__ lengths, int compute, Chunks w,
+                                                    const int32_t *__restrict__ lengths, int tiles, Chunks w,
                                                     const float *state_in, E *__restrict__ out, float *state_out,
                                                     Kept kept) {
     using F = Blob<E, DS, STATES>;
-    constexpr int C = F::C, MT = F::MT, NT = F::NT, GP = F::GP, NP = F::NP;
+    using M = ScanLds<E, DS, KS, STATES>;
+    constexpr int C = F::C, MT = F::MT, NT = F::NT, GP = F::GP, NP = F::NP, DW = DS / KS;
     extern __shared__ char lds[];
     const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, gr = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+    const int tile = wv / KS, part = wv % KS, s0 = part * DW;  // the wave's columns and groups of dk
     const int bh = head_of(blockIdx.x, gridDim.x), b = bh / a.Hv, h = bh % a.Hv, hk = h / (a.Hv / a.Hk);
     const int n = lengths ? max(0, min(a.L, lengths[b])) : a.L, nc = (n + C - 1) / C;
-    const int col = ((int)blockIdx.y * compute + wv) * 16 + m;
-    const bool mine = wv < compute && col - m < (STATES ? kept.dvp : a.dv), live = mine && col < a.dv;
-    const int64_t s0 = (int64_t)bh * a.dk * a.dv + col;
+    const int col = ((int)blockIdx.y * tiles + tile) * 16 + m;
+    const bool mine = tile < tiles && col - m < (STATES ? kept.dvp : a.dv), live = mine && col < a.dv;
     const char *key = w.key + ((int64_t)b * a.Hk + hk) * w.NC * F::KEY;
     const char *head = w.head + (int64_t)bh * w.NC * F::HEAD;
-    f32x4 S[2 * DS];
+    f32x4 S[2 * DW];
 #pragma unroll
-    for (int t = 0; t < 2 * DS; ++t) S[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < 2 * DW; ++t) S[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
     if (state_in) {
         const float *from = state_in + (int64_t)bh * a.dk * a.dv + min(col, a.dv - 1);
 #pragma unroll
-        for (int t = 0; t < 2 * DS; ++t)
+        for (int t = 0; t < 2 * DW; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) S[t][r] = from[(int64_t)min(16 * t + 4 * gr + r, a.dk - 1) * a.dv];
+            for (int r = 0; r < 4; ++r) S[t][r] = from[(int64_t)min(dk_of(2 * s0 + t, 4 * gr + r), a.dk - 1) * a.dv];
 #pragma unroll
-        for (int t = 0; t < 2 * DS; ++t)
+        for (int t = 0; t < 2 * DW; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) S[t][r] = live && 16 * t + 4 * gr + r < a.dk ? S[t][r] : 0.0f;
+            for (int r = 0; r < 4; ++r) S[t][r] = live && dk_of(2 * s0 + t, 4 * gr + r) < a.dk ? S[t][r] : 0.0f;
     }
-    auto fetch = [&](int c) {
-        char *dst = lds + (c % NBUF) * F::SCAN;
-        to_lds(dst, key + (int64_t)c * F::KEY, F::SCAN_KEY, wv, waves, lane);
-        to_lds(dst + F::SCAN_KEY, head + (int64_t)c * F::HEAD, F::SCAN_HEAD, wv, waves, lane);
+    auto fetch_k = [&](int c) { to_lds(lds + (c % M::KB) * F::K, key + (int64_t)c * F::KEY, F::K, wv, waves, lane); };
+    auto fetch_q = [&](int c) {
+        if (!STATES) to_lds(lds + M::AT_Q, key + (int64_t)c * F::KEY + F::K, F::K, wv, waves, lane);
+    };
+    auto fetch_t = [&](int c) {
+        to_lds(lds + M::AT_TP + (c % M::TB) * M::TP, head + (int64_t)c * F::HEAD, M::TP, wv, waves, lane);
     };
     // sample i of the chunk, column col: uniform rows and the lane's offset within four of them
     const int64_t vstep = (int64_t)a.Hv * a.dv;
     const E *vrow = v + ((int64_t)b * a.L * a.Hv + h) * a.dv;
     E *orow = out + ((int64_t)b * a.L * a.Hv + h) * a.dv;
     const uint32_t lin = (uint32_t)((4 * gr * vstep + min(col, a.dv - 1)) * sizeof(E)),
-                   lout = (uint32_t)((4 * gr * vstep + col) * sizeof(E));
+                   lout = (uint32_t)((4 * gr * vstep + col) * sizeof(E)),
+                   lkept = (uint32_t)(4 * gr * kept.dvp + col) * 4, lstate = (uint32_t)(8 * gr * kept.dvp + col) * 4;
     E vv[MT][4];
     auto values = [&](int c) {
         const E *p = vrow + (int64_t)c * C * vstep;
@@ -366,11 +365,53 @@ __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Arg
     };
     if (nc) {
         values(0);
-        fetch(0);
+        fetch_k(0);
+        fetch_q(0);
+        fetch_t(0);
         wait_copies();
     }
     __syncthreads();
     for (int c = 0; c < nc; ++c) {
+        const char *K = lds + (c % M::KB) * F::K, *Q = lds + M::AT_Q, *T = lds + M::AT_TP + (c % M::TB) * M::TP,
+                   *P = T + F::PAT;
+        const float *co = reinterpret_cast<const float *>(T + F::T);
+        f32x4 X[MT], Y[MT];
+        if (mine) {
+            if (STATES) {
+                float *dst = kept.S + ((int64_t)bh * w.NC + c) * 32 * DS * kept.dvp;
+#pragma unroll
+                for (int t = 0; t < 2 * DW; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        at(dst + (32 * (s0 + (t >> 1)) + 4 * (t & 1) + r) * kept.dvp, lstate) = S[t][r];
+            }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) X[mt] = Y[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < DW; ++s) {
+                const Terms<3> st = split<3>(S[2 * s], S[2 * s + 1]);
+                Terms<NP> sp;
+#pragma unroll
+                for (int i = 0; i < NP; ++i) sp.t[i] = st.t[i];
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    mma<NT, 3>(X[mt], frag<NT>(K + (mt * DS + s0 + s) * NT * FRAG, lane), st);
+                    if (!STATES) mma<NT, NP>(Y[mt], frag<NT>(Q + (mt * DS + s0 + s) * NT * FRAG, lane), sp);
+                }
+            }
+            if (KS > 1) {
+                char *xb = lds + M::AT_X + tile * KS * MT * FRAG, *yb = lds + M::AT_Y + tile * MT * (KS - 1) * FRAG;
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    *reinterpret_cast<f32x4 *>(xb + (part * MT + mt) * FRAG + lane * 16) = X[mt];
+                    const int own = mt * KS / MT;  // finishes these rows of out
+                    if (!STATES && part != own)
+                        *reinterpret_cast<f32x4 *>(yb + (mt * (KS - 1) + part - (part > own)) * FRAG + lane * 16) = Y[mt];
+                }
+            }
+        }
+        if (M::TB == 1) wait_copies();  // (T and P of this chunk)
+        lds_barrier();
         float vc[MT][4];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
@@ -381,34 +422,21 @@ __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Arg
             }
         if (c + 1 < nc) {
             values(c + 1);
-            if (NBUF == 2) fetch(c + 1);
+            fetch_q(c + 1);
+            if (M::KB == 2) fetch_k(c + 1);
+            if (M::TB == 2) fetch_t(c + 1);
         }
-        f32x4 Y[MT];
         if (mine) {
-            const char *K = lds + (c % NBUF) * F::SCAN, *KT = K + F::K, *Q = KT + F::KT, *T = K + F::SCAN_KEY,
-                       *P = T + F::PAT;
-            const float *co = reinterpret_cast<const float *>(T + F::T);
-            if (STATES) {
-                float *dst = kept.S + ((int64_t)bh * w.NC + c) * 32 * DS * kept.dvp;
-                const uint32_t lo = (uint32_t)(4 * gr * kept.dvp + col) * 4;
-#pragma unroll
-                for (int t = 0; t < 2 * DS; ++t)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) at(dst + (16 * t + r) * kept.dvp, lo) = S[t][r];
-            }
-            f32x4 X[MT];
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) X[mt] = Y[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int s = 0; s < DS; ++s) {
-                const Terms<3> st = split<3>(S[2 * s], S[2 * s + 1]);
-                Terms<NP> sp;
-#pragma unroll
-                for (int i = 0; i < NP; ++i) sp.t[i] = st.t[i];
+            if (KS > 1) {
+                const char *xb = lds + M::AT_X + tile * KS * MT * FRAG;
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {
-                    mma<NT, 3>(X[mt], frag<NT>(K + (mt * DS + s) * NT * FRAG, lane), st);
-                    if (!STATES) mma<NT, NP>(Y[mt], frag<NT>(Q + (mt * DS + s) * NT * FRAG, lane), sp);
+                    f32x4 x[KS];
+#pragma unroll
+                    for (int p = 0; p < KS; ++p) x[p] = *reinterpret_cast<const f32x4 *>(xb + (p * MT + mt) * FRAG + lane * 16);
+#pragma unroll
+                    for (int p = 1; p < KS; ++p) x[0] += x[p];
+                    X[mt] = x[0];
                 }
             }
             f32x4 U[MT];
@@ -417,9 +445,7 @@ __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Arg
                 const f32x4 ev = *reinterpret_cast<const f32x4 *>(co + 16 * mt + 4 * gr);
                 const f32x4 be = *reinterpret_cast<const f32x4 *>(co + C + 16 * mt + 4 * gr);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    X[mt][r] = be[r] * (vc[mt][r] - ev[r] * X[mt][r]);
-                }
+                for (int r = 0; r < 4; ++r) X[mt][r] = be[r] * (vc[mt][r] - ev[r] * X[mt][r]);
                 U[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
             }
 #pragma unroll
@@ -428,83 +454,119 @@ __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Arg
 #pragma unroll
                 for (int mt = 2 * gp; mt < MT; ++mt) mma<3, 3>(U[mt], frag<3>(T + F::lower(mt, gp) * 3 * FRAG, lane), rt);
             }
+            if (!STATES) {  // out
+                const char *yb = lds + M::AT_Y + tile * MT * (KS - 1) * FRAG;
+                Terms<NP> ut[GP];
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-                if (!STATES) Y[mt] *= *reinterpret_cast<const f32x4 *>(co + 3 * C + 16 * mt + 4 * gr);
-            if (STATES) {
+                for (int gp = 0; gp < GP; ++gp) ut[gp] = split<NP>(U[2 * gp], U[2 * gp + 1]);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    if (part != mt * KS / MT) continue;
+#pragma unroll
+                    for (int p = 0; p < KS - 1; ++p)
+                        Y[mt] += *reinterpret_cast<const f32x4 *>(yb + (mt * (KS - 1) + p) * FRAG + lane * 16);
+                    Y[mt] *= *reinterpret_cast<const f32x4 *>(co + 3 * C + 16 * mt + 4 * gr);
+#pragma unroll
+                    for (int gp = 0; gp <= mt / 2; ++gp)
+                        mma<NP, NP>(Y[mt], frag<NP>(P + F::lower(mt, gp) * NP * FRAG, lane), ut[gp]);
+                }
+            } else {
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) Y[mt] = U[mt];
             }
             const float end = co[C - 1];  // E of the last sample
 #pragma unroll
-            for (int t = 0; t < 2 * DS; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) S[t][r] *= end;
+            for (int t = 0; t < 2 * DW; ++t) S[t] *= end;
 #pragma unroll
             for (int gp = 0; gp < GP; ++gp) {
-                if (!STATES) {
-                    const Terms<NP> ut = split<NP>(U[2 * gp], U[2 * gp + 1]);
-#pragma unroll
-                    for (int mt = 2 * gp; mt < MT; ++mt)
-                        mma<NP, NP>(Y[mt], frag<NP>(P + F::lower(mt, gp) * NP * FRAG, lane), ut);
-                }
                 const f32x4 l0 = *reinterpret_cast<const f32x4 *>(co + 2 * C + 32 * gp + 4 * gr);
                 const f32x4 l1 = *reinterpret_cast<const f32x4 *>(co + 2 * C + 32 * gp + 16 + 4 * gr);
                 const Terms<3> lt = split<3>(U[2 * gp] * l0, U[2 * gp + 1] * l1);
 #pragma unroll
-                for (int t = 0; t < 2 * DS; ++t)
-                    mma<NT, 3>(S[t], frag<NT>(KT + (t * GP + gp) * NT * FRAG, lane), lt);
+                for (int t = 0; t < 2 * DW; ++t) mma<NT, 3>(S[t], tfrag<NT, DS>(K, 2 * s0 + t, gp, lane), lt);
             }
         }
-        // the next chunk's operands have come; what is stored now has a chunk's time to get out
-        if (NBUF == 2) wait_copies();
-        __syncthreads();
-        if (NBUF == 1 && c + 1 < nc) fetch(c + 1);
+        // the next chunk's operands have come; what is stored now has half a chunk's time to get out
+        wait_copies();
+        lds_barrier();
+        if (c + 1 < nc) {
+            if (M::KB == 1) fetch_k(c + 1);
+            if (M::TB == 1) fetch_t(c + 1);
+        }
         if (STATES && mine) {
             float *dst = kept.U + ((int64_t)bh * w.NC + c) * C * kept.dvp;
-            const uint32_t lo = (uint32_t)(4 * gr * kept.dvp + col) * 4;
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+            for (int mt = 0; mt < MT; ++mt) {
+                if (part != mt * KS / MT) continue;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) at(dst + (16 * mt + r) * kept.dvp, lo) = Y[mt][r];
+                for (int r = 0; r < 4; ++r) at(dst + (16 * mt + r) * kept.dvp, lkept) = Y[mt][r];
+            }
         }
         if (!STATES && live) {
             E *p = orow + (int64_t)c * C * vstep;
-            if ((c + 1) * C <= n) {
+            const bool full = (c + 1) * C <= n;
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
+            for (int mt = 0; mt < MT; ++mt) {
+                if (part != mt * KS / MT) continue;
+                if (full) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) at(p + (16 * mt + r) * vstep, lout) = from_float<E>(Y[mt][r]);
-            } else {
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
+                } else {
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
                         if (c * C + 16 * mt + 4 * gr + r < n) at(p + (16 * mt + r) * vstep, lout) = from_float<E>(Y[mt][r]);
+                }
             }
         }
-        if (NBUF == 1) {
+        if (M::KB == 1 && c + 1 < nc) {
             wait_copies();
-            __syncthreads();
+            lds_barrier();
         }
     }
     if (!live || !state_out) return;
 #pragma unroll
-    for (int t = 0; t < 2 * DS; ++t)
+    for (int t = 0; t < 2 * DW; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int d = 16 * t + 4 * gr + r;
-            if (d < a.dk) state_out[s0 + (int64_t)d * a.dv] = S[t][r];
+            const int d = dk_of(2 * s0 + t, 4 * gr + r);
+            if (d < a.dk) state_out[(int64_t)bh * a.dk * a.dv + (int64_t)d * a.dv + col] = S[t][r];
         }
 }
 
-// Waves of a workgroup that carry columns, for `tiles` of 16 columns a head: up
-// to eight share the operands, fewer where the workgroups would not fill the CUs.
-inline int scan_waves(const Args &a, int tiles) {
-    int n = tiles < 8 ? tiles : 8;
-    while (n > 1 && (int64_t)a.B * a.Hv * ((tiles + n - 1) / n) < 256) n = (n + 1) / 2;
-    return n;
+// How a call's columns go to waves: KS waves to a tile of 16 columns and `tiles`
+// of them a workgroup (`threads` in all), out of `all` tiles a head.
+struct Cols {
+    int KS, tiles, blocks, threads;
+};
+inline Cols columns(const Args &a, int all, int DS) {
+    Cols c;
+    const int64_t waves = (int64_t)a.B * a.Hv * all;
+    c.KS = 1;
+    while (c.KS < 4 && 2 * c.KS <= DS && waves * c.KS <= 1024) c.KS *= 2;  // up to two waves on each of 1024 SIMDs
+    c.tiles = all < 8 / c.KS ? all : 8 / c.KS;
+    while (c.tiles > 1 && (int64_t)a.B * a.Hv * ((all + c.tiles - 1) / c.tiles) < 256) c.tiles = (c.tiles + 1) / 2;
+    c.blocks = (all + c.tiles - 1) / c.tiles;
+    c.threads = 64 * (c.tiles * c.KS > 4 ? c.tiles * c.KS : 4);
+    return c;
 }
+
+template <class E, int DS, int KS, bool STATES>
+void launch_scan(const Cols &cols, const void *v, const Args &a, const int32_t *lengths, const Chunks &w,
+                 const float *state_in, void *out, float *state_out, const Kept &kept, hipStream_t st) {
+    constexpr int LDS = ScanLds<E, DS, KS, STATES>::BYTES;
+    hipLaunchKernelGGL((k_delta_scan<E, DS, KS, STATES>), dim3((unsigned)(a.B * a.Hv), (unsigned)cols.blocks),
+                       dim3((unsigned)cols.threads), LDS, st, static_cast<const E *>(v), a, lengths, cols.tiles, w, state_in,
+                       static_cast<E *>(out), state_out, kept);
+}
+// CALL(KS) with the form that `cols` asks for
+#define SPK_DELTA_PARTS(DS, cols, CALL)      \
+    if (DS >= 4 && (cols).KS == 4) {         \
+        CALL((DS >= 4 ? 4 : 1));             \
+    } else if (DS >= 2 && (cols).KS == 2) {  \
+        CALL((DS >= 2 ? 2 : 1));             \
+    } else {                                 \
+        CALL(1);                             \
+    }
 
 inline int groups_of(int dk) {
     const int d = (dk + 31) / 32;
@@ -519,10 +581,10 @@ inline int groups_of(int dk) {
         default: CALL(8);                         \
     }
 
-// Whether rows of dk elements can be read four at a time.
+// Whether rows of dk elements can be read eight at a time.
 template <class E>
 int wide_rows(int dk, const void *q, const void *k) {
-    return dk % 4 == 0 && ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k)) & (4 * sizeof(E) - 1)) == 0;
+    return dk % 8 == 0 && aligned16(q) && aligned16(k);
 }
 
 }  // namespace delta
