@@ -113,7 +113,8 @@ SPK_API int spk_delta_rule_backward(const void *q, const void *k, const void *v,
  * fraction bits, so that sums do not depend on their order: repeated calls
  * give the same winners.
  * Limits: 0 <= temperature < inf, 0 <= top_k, 0 < top_p <= 1,
- * 0 <= min_p <= 1, 1 <= T <= 255, C*H*W <= 2^24, B <= 2^21.
+ * 0 <= min_p <= 1, 1 <= T <= 255, C*H*W <= 2^24, B <= 2^21 (65535
+ * where C*H*W > 16384).
  * Workspace: spk_sample_winners_workspace_size(...) bytes.                  */
 SPK_API size_t spk_sample_winners_workspace_size(int dtype, int B, int C, int H, int W);
 SPK_API int spk_sample_winners(const void *scores, int dtype, const uint8_t *t_first, const float *u, int B, int T,

@@ -8,10 +8,11 @@
 // 64-bit fixed-point numbers, so that sums do not depend on the order of the
 // histogram's atomics, nor of anything else.
 //
-// Rows of up to 16 keys a thread stay in registers.  Longer ones are read again
-// for each step (largest score; histogram; the boundary's own bin into LDS; sums
-// by index): a step is bound by reading the row, and beside it the weights cost
-// some 20 double-precision instructions a score.
+// Rows of up to 16 keys a thread stay in registers.  Longer ones go through
+// launches of several workgroups a row (largest score; histogram; the keys of the
+// boundary's bin; sums by index; the draw), each reading the row again: a step is
+// bound by reading the row, and where it weighs scores by some 30 instructions for
+// each, half of them in double precision.
 #include <cmath>
 
 #include "common.hpp"
@@ -67,12 +68,11 @@ constexpr int LIST = 4096;  // keys of one bin that LDS takes
 // (r ln 2)^6 / 720, is below 4e-17.  The largest itself (also +inf) weighs 2^shift.
 struct Weigher {
     double top, per, shift_d;
-    uint32_t ktop;
     int shift;
     const double *pow;
-    __device__ __forceinline__ uint64_t operator()(uint32_t k) const {
-        if (k == ktop) return 1ull << shift;
-        const double y = fmax(fma((double)value_of(k) - top, per, shift_d), -1.0);
+    __device__ __forceinline__ uint64_t operator()(uint32_t k) const { return of(value_of(k)); }
+    __device__ __forceinline__ uint64_t of(float v) const {
+        const double y = fmax(fma((double)v - top, per, shift_d), -1.0);
         const double n = floor(y), f = y - n;
         const int j = (int)(f * POW);
         const double t = (f - j * (1.0 / POW)) * 0.69314718055994530942;
@@ -86,7 +86,7 @@ struct Weigher {
         const int e = (int)n + (int)(bits >> 52) - 1023 - 52;
         const uint64_t sig = (bits & 0xFFFFFFFFFFFFFull) | 0x10000000000000ull;
         const uint64_t w = e >= 0 ? sig << e : sig >> -e;
-        return y >= 0.0 ? w : 0ull;
+        return (double)v == top ? 1ull << shift : y >= 0.0 ? w : 0ull;
     }
 };
 
@@ -200,7 +200,6 @@ template <int WAVES>
 __device__ __forceinline__ Weigher weigher(Shared<WAVES> &sh, const SampleArgs &a, uint32_t ktop) {
     if (threadIdx.x < POW) sh.pow[threadIdx.x] = exp2(threadIdx.x * (1.0 / POW));
     Weigher w;
-    w.ktop = ktop;
     w.top = (double)value_of(ktop);
     w.per = a.temperature > 0.0f ? 1.4426950408889634074 / (double)a.temperature : 0.0;
     w.shift = a.shift;
@@ -380,220 +379,444 @@ __global__ __launch_bounds__(WAVES * 64) void k_sample_short(const E *__restrict
 }
 
 constexpr int LONG_WAVES = 16, LONG_THREADS = LONG_WAVES * 64;
+constexpr int SPLITS = 64;  // workgroups of a row at most
 
-// Calls f(key, index) for the keys i0 <= index < i1 of a row, by `threads`
+// Calls f(score, index) for the indices i0 <= index < i1 of a row, by `threads`
 // threads of which this is number `t`: vectors of 16 bytes, four in flight a
-// thread, and the ends that no whole vector covers one by one.  A key that
-// cannot win is 0.
+// thread, and the ends that no whole vector covers one by one.  A masked score
+// is -infinity.
 template <class E, class F>
 __device__ __forceinline__ void for_row(const E *x, const uint8_t *tf, int T, int64_t i0, int64_t i1, int t, int threads,
                                         F f) {
     constexpr int V = 16 / sizeof(E), UNR = 4;
-    auto one = [&](int64_t i) {
-        f(tf && tf[i] >= T ? 0u : key_of(as_float<E>(x[i])), i);
-    };
     const int64_t skip = (V - (int64_t)((reinterpret_cast<uintptr_t>(x + i0) / sizeof(E)) % V)) % V;
-    const int64_t v0 = min(i1, i0 + skip), nv = (i1 - v0) / V;
+    const int64_t v0 = min(i1, i0 + skip);
+    const int nv = (int)((i1 - v0) / V);
     struct alignas(16) Vec {
         E e[V];
     };
     const Vec *xv = reinterpret_cast<const Vec *>(x + v0);
-    for (int64_t j = t; j < nv; j += (int64_t)threads * UNR) {
+    for (int j = t; j < nv; j += threads * UNR) {
         Vec r[UNR];
+        uint8_t tt[UNR][V];
 #pragma unroll
-        for (int q = 0; q < UNR; ++q) r[q] = xv[min(j + (int64_t)q * threads, nv - 1)];
+        for (int q = 0; q < UNR; ++q) r[q] = xv[min(j + q * threads, nv - 1)];
         if (tf) {
-            uint8_t tt[UNR][V];
 #pragma unroll
             for (int q = 0; q < UNR; ++q)
 #pragma unroll
-                for (int c = 0; c < V; ++c) tt[q][c] = tf[v0 + min(j + (int64_t)q * threads, nv - 1) * V + c];
+                for (int c = 0; c < V; ++c) tt[q][c] = tf[v0 + (int64_t)min(j + q * threads, nv - 1) * V + c];
+        }
 #pragma unroll
-            for (int q = 0; q < UNR; ++q)
-                if (j + (int64_t)q * threads < nv)
+        for (int q = 0; q < UNR; ++q) {
+            if (j + q * threads >= nv) break;
 #pragma unroll
-                    for (int c = 0; c < V; ++c)
-                        f(tt[q][c] < T ? key_of(as_float<E>(r[q].e[c])) : 0u, v0 + (j + (int64_t)q * threads) * V + c);
-        } else {
-#pragma unroll
-            for (int q = 0; q < UNR; ++q)
-                if (j + (int64_t)q * threads < nv)
-#pragma unroll
-                    for (int c = 0; c < V; ++c)
-                        f(key_of(as_float<E>(r[q].e[c])), v0 + (j + (int64_t)q * threads) * V + c);
+            for (int c = 0; c < V; ++c) {
+                const float v = as_float<E>(r[q].e[c]);
+                f(tf && tt[q][c] >= T ? -INFINITY : v, v0 + (int64_t)(j + q * threads) * V + c);
+            }
         }
     }
-    const int64_t head = v0 - i0, tail = i1 - v0 - nv * V;  // below V each
-    if (t < head) one(i0 + t);
-    else if (t - head < tail) one(i1 - tail + (t - head));
+    const int64_t head = v0 - i0, tail = i1 - v0 - (int64_t)nv * V;  // below V each
+    if (t < head + tail) {
+        const int64_t i = t < head ? i0 + t : i1 - tail + (t - head);
+        const float v = as_float<E>(x[i]);
+        f(tf && tf[i] >= T ? -INFINITY : v, i);
+    }
 }
 
-// Grid: one workgroup per image of any size.  A boundary is looked for in a
-// histogram of BINS equal steps of the score below the largest (1/64 of the
-// temperature each, the rest in the last), then among the keys of its bin, in
-// LDS where they fit; else by reading the row again for every digit.
+// Workspace of long rows: each step is a launch of `splits` workgroups a row.
+struct RowPart {
+    float top, low;  // largest and smallest score that can win
+    uint32_t n;      // how many can
+};
+struct RowSums {
+    uint64_t kept, equal;  // weight above the edge, keys equal to it
+};
+struct RowEdge {
+    uint64_t equal;
+    uint32_t edge, any;
+};
+struct Work {
+    int splits;
+    uint64_t *hist;   // [B][BINS]
+    uint32_t *list;   // [B][LIST]
+    uint32_t *count;  // [B]
+    RowPart *part;    // [B][splits]
+    RowSums *sums;    // [B][splits][LONG_WAVES]
+    RowEdge *edge;    // [B]
+};
+
+// A long row's scores and the workgroup's share of them.
 template <class E>
-__global__ __launch_bounds__(LONG_THREADS) void k_sample_long(const E *__restrict__ scores,
+struct LongRow {
+    const E *x;
+    const uint8_t *tf;
+    int64_t N, i0, i1, seg;
+    int T;
+    __device__ __forceinline__ LongRow(const E *scores, const uint8_t *t_first, const SampleArgs &a, int splits, int64_t b,
+                                       int split)
+        : x(scores + b * a.N), tf(t_first ? t_first + b * a.N : nullptr), N(a.N), T(a.T) {
+        seg = ((N + (int64_t)splits * LONG_WAVES - 1) / ((int64_t)splits * LONG_WAVES) + 7) / 8 * 8;  // of a wave
+        i0 = min(N, split * LONG_WAVES * seg);
+        i1 = min(N, i0 + LONG_WAVES * seg);
+    }
+    template <class F>
+    __device__ __forceinline__ void own(F f) const { for_row<E>(x, tf, T, i0, i1, threadIdx.x, LONG_THREADS, f); }
+    template <class F>
+    __device__ __forceinline__ void all(F f) const { for_row<E>(x, tf, T, 0, N, threadIdx.x, LONG_THREADS, f); }
+};
+
+// What a row's parts add up to, and the bins of its histogram: equal steps of
+// the score from the largest down to the smallest, or to where weights end.
+struct RowStat {
+    float top, steps;
+    uint32_t n;
+    __device__ __forceinline__ RowStat(const RowPart *part, int splits, float temperature) {
+        const int lane = threadIdx.x & 63;
+        const RowPart p = part[min(lane, splits - 1)];
+        float hi = p.top, lo = p.low;
+        int m = lane < splits ? (int)p.n : 0;
+#pragma unroll
+        for (int s = 32; s >= 1; s >>= 1) {
+            hi = fmaxf(hi, __shfl_xor(hi, s, 64));
+            lo = fminf(lo, __shfl_xor(lo, s, 64));
+            m += __shfl_xor(m, s, 64);
+        }
+        top = hi;
+        n = (uint32_t)m;
+        steps = (float)(BINS - 2) / fmaxf(fminf(hi - lo, 44.0f * temperature), 1e-30f);
+    }
+    __device__ __forceinline__ int bin(float v) const {  // does not fall as the score falls
+        return v == top ? 0 : (int)fminf((top - v) * steps, (float)(BINS - 1));
+    }
+};
+
+__device__ __forceinline__ bool wins(float v) { return v > -INFINITY; }  // (false for NaN)
+
+template <class E>
+__global__ __launch_bounds__(LONG_THREADS) void k_sample_top(const E *__restrict__ scores,
+                                                             const uint8_t *__restrict__ t_first, SampleArgs a, Work w) {
+    __shared__ RowPart sh[LONG_WAVES];
+    const int64_t b = blockIdx.y;
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    for (int i = blockIdx.x * LONG_THREADS + threadIdx.x; i < BINS; i += gridDim.x * LONG_THREADS) w.hist[b * BINS + i] = 0;
+    if (blockIdx.x == 0 && threadIdx.x == 0) w.count[b] = 0;
+    const LongRow<E> row(scores, t_first, a, w.splits, b, blockIdx.x);
+    float hi = -INFINITY, lo = INFINITY;
+    int n = 0;
+    row.own([&](float v, int64_t) {
+        hi = fmaxf(hi, v);  // (the other one where one is NaN)
+        lo = fminf(lo, wins(v) ? v : INFINITY);
+        n += wins(v);
+    });
+#pragma unroll
+    for (int s = 32; s >= 1; s >>= 1) {
+        hi = fmaxf(hi, __shfl_xor(hi, s, 64));
+        lo = fminf(lo, __shfl_xor(lo, s, 64));
+        n += __shfl_xor(n, s, 64);
+    }
+    if (lane == 0) sh[wv] = RowPart{hi, lo, (uint32_t)n};
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        RowPart p = sh[0];
+        for (int q = 1; q < LONG_WAVES; ++q) {
+            p.top = fmaxf(p.top, sh[q].top);
+            p.low = fminf(p.low, sh[q].low);
+            p.n += sh[q].n;
+        }
+        w.part[b * w.splits + blockIdx.x] = p;
+    }
+}
+
+// The row's histogram, of counts or of weights.
+template <class E, bool COUNT>
+__global__ __launch_bounds__(LONG_THREADS) void k_sample_hist(const E *__restrict__ scores,
+                                                              const uint8_t *__restrict__ t_first, SampleArgs a, Work w) {
+    __shared__ Shared<LONG_WAVES> sh;
+    const int64_t b = blockIdx.y;
+    const RowStat st(w.part + b * w.splits, w.splits, a.temperature);
+    if (st.n == 0) return;
+    const Weigher weigh = weigher<LONG_WAVES>(sh, a, key_of(st.top));
+    for (int i = threadIdx.x; i < BINS; i += LONG_THREADS) sh.hist[i] = 0;
+    __syncthreads();
+    const LongRow<E> row(scores, t_first, a, w.splits, b, blockIdx.x);
+    row.own([&](float v, int64_t) {
+        const uint64_t x = COUNT ? 1 : weigh.of(v);
+        if (wins(v) && x) atomicAdd((unsigned long long *)&sh.hist[st.bin(v)], (unsigned long long)x);
+    });
+    __syncthreads();
+    for (int i = threadIdx.x; i < BINS; i += LONG_THREADS)
+        if (sh.hist[i]) atomicAdd((unsigned long long *)&w.hist[b * BINS + i], (unsigned long long)sh.hist[i]);
+}
+
+// The boundary's bin of the row's histogram and what lies before it.
+template <bool COUNT>
+__device__ __forceinline__ int boundary_bin(Shared<LONG_WAVES> &sh, const SampleArgs &a, const Work &w, int64_t b,
+                                            uint64_t *want, uint64_t *over) {
+    uint64_t sum = 0;
+    for (int i = threadIdx.x; i < BINS; i += LONG_THREADS) sum += sh.hist[i] = w.hist[b * BINS + i];
+    sum = block_sum<LONG_WAVES>(sh, sum);
+    *want = COUNT ? (uint64_t)a.top_k : share(a.top_p, sum);
+    return (int)find_bin<LONG_WAVES>(sh, BINS, *want, over);
+}
+
+// The keys of the boundary's bin; with COUNT those of the bins before it too, so
+// that what step 1 keeps is all there.
+template <class E, bool COUNT>
+__global__ __launch_bounds__(LONG_THREADS) void k_sample_list(const E *__restrict__ scores,
+                                                              const uint8_t *__restrict__ t_first, SampleArgs a, Work w) {
+    __shared__ Shared<LONG_WAVES> sh;
+    const int64_t b = blockIdx.y;
+    const RowStat st(w.part + b * w.splits, w.splits, a.temperature);
+    if (st.n == 0) return;
+    uint64_t want, over;
+    const int bin = boundary_bin<COUNT>(sh, a, w, b, &want, &over);
+    const LongRow<E> row(scores, t_first, a, w.splits, b, blockIdx.x);
+    row.own([&](float v, int64_t) {
+        if (!wins(v)) return;
+        const int at_bin = st.bin(v);
+        if (at_bin == bin || (COUNT && at_bin < bin)) {
+            const uint32_t at = atomicAdd(&w.count[b], 1u);
+            if (at < LIST) w.list[b * LIST + at] = key_of(v);
+        }
+    });
+}
+
+// The boundary (each workgroup of the row finds it for itself), then the sums of
+// the waves' segments.  FORM: 0 nothing is cut, or all but the largest; 1 by
+// weight; 2 by count, then by weight.
+template <class E, int FORM>
+__global__ __launch_bounds__(LONG_THREADS) void k_sample_sums(const E *__restrict__ scores,
+                                                              const uint8_t *__restrict__ t_first, SampleArgs a, Work w) {
+    constexpr int WAVES = LONG_WAVES;
+    __shared__ Shared<WAVES> sh;
+    const int64_t b = blockIdx.y;
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    const RowStat st(w.part + b * w.splits, w.splits, a.temperature);
+    if (st.n == 0) {
+        if (blockIdx.x == 0 && tid == 0) w.edge[b].any = 0;
+        return;
+    }
+    const uint32_t ktop = key_of(st.top);
+    const Weigher weigh = weigher<WAVES>(sh, a, ktop);
+    const LongRow<E> row(scores, t_first, a, w.splits, b, blockIdx.x);
+    __syncthreads();
+    Edge e;
+    if (FORM == 0) {
+        if (a.temperature == 0.0f || a.top_k == 1) {
+            e.edge = ktop;
+            e.equal = 1;
+        }
+    } else {
+        uint64_t want = 0, over = 0, above;
+        if (FORM == 1) boundary_bin<false>(sh, a, w, b, &want, &over);
+        const uint32_t n = w.count[b];
+        const bool listed = n <= LIST;
+        if (listed) {
+            for (uint32_t i = tid; i < n; i += LONG_THREADS) sh.list[i] = w.list[b * LIST + i];
+            __syncthreads();
+        }
+        // f(key, value()) for the keys from the edge up: of the list, else of the whole row
+        auto each = [&](auto f, auto value) {
+            if (listed) {
+                for (uint32_t i = tid; i < n; i += LONG_THREADS) {
+                    const uint32_t k = sh.list[i];
+                    if (k >= e.edge) f(k, [&] { return value(k); });
+                }
+            } else {
+                row.all([&](float v, int64_t) {
+                    const uint32_t k = key_of(v);
+                    if (k >= e.edge && k != 0) f(k, [&] { return value(k); });
+                });
+            }
+        };
+        auto one = [](uint32_t) { return (uint64_t)1; };
+        if (FORM == 1) {
+            // (the list is the boundary's bin alone; the row stands for all bins)
+            const uint64_t rest = listed ? want - over : want;
+            const uint32_t k = descend<WAVES>(sh, rest, [&](auto f) { each(f, weigh); }, &above);
+            e.by_weight(k, rest, above, weigh(k));
+        } else {
+            if ((uint64_t)a.top_k < st.n) {
+                const uint32_t k = descend<WAVES>(sh, (uint64_t)a.top_k, [&](auto f) { each(f, one); }, &above);
+                e.equal = (uint64_t)a.top_k - above;
+                e.edge = k;
+            }
+            if (a.top_p < 1.0f) {
+                uint64_t sum = 0;
+                each([&](uint32_t k, auto value) {
+                    if (k > e.edge || e.equal == ~0ull) sum += value();
+                }, weigh);
+                sum = block_sum<WAVES>(sh, sum);
+                if (e.equal != ~0ull) sum += e.equal * weigh(e.edge);
+                want = share(a.top_p, sum);
+                // (the edge takes part with all its equals: one that step 1 cut has its own limit)
+                const uint32_t k = descend<WAVES>(sh, want, [&](auto f) { each(f, weigh); }, &above);
+                e.by_weight(k, want, above, weigh(k));
+            }
+        }
+    }
+    const uint64_t min_w = (uint64_t)ceil(ldexp((double)a.min_p, a.shift));
+    const float edge = e.edge > 1 ? value_of(e.edge) : -INFINITY;  // (1: everything that can win is above)
+    uint64_t sum = 0;
+    uint32_t eqs = 0;
+    const int64_t s0 = min(row.i1, row.i0 + wv * row.seg), s1 = min(row.i1, s0 + row.seg);
+    for_row<E>(row.x, row.tf, row.T, s0, s1, lane, 64, [&](float v, int64_t) {
+        if (v > edge) {
+            const uint64_t x = weigh.of(v);
+            sum += x >= min_w ? x : 0;
+        }
+        eqs += v == edge && wins(v);
+    });
+    sum = wave_sum_u64(sum);
+    const uint64_t eqn = wave_sum_u64(eqs);
+    if (lane == 0) w.sums[(b * w.splits + blockIdx.x) * WAVES + wv] = RowSums{sum, eqn};
+    if (blockIdx.x == 0 && tid == 0) w.edge[b] = RowEdge{e.equal, e.edge, 1};
+}
+
+// Grid: one workgroup per row: the segment of the draw, then the winner in it.
+template <class E>
+__global__ __launch_bounds__(LONG_THREADS) void k_sample_pick(const E *__restrict__ scores,
                                                               const uint8_t *__restrict__ t_first,
-                                                              const float *__restrict__ u, SampleArgs a,
+                                                              const float *__restrict__ u, SampleArgs a, Work w,
                                                               int32_t *__restrict__ winners,
                                                               int32_t *__restrict__ n_win) {
     constexpr int WAVES = LONG_WAVES;
     __shared__ Shared<WAVES> sh;
-    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t b = blockIdx.x, N = a.N;
-    const E *x = scores + b * N;
-    const uint8_t *tf = t_first ? t_first + b * N : nullptr;
-    auto each = [&](auto f) { for_row<E>(x, tf, a.T, 0, N, tid, LONG_THREADS, f); };
-    uint32_t mx = 0, c32 = 0;
-    each([&](uint32_t k, int64_t) {
-        mx = k > mx ? k : mx;
-        c32 += k != 0;
-    });
-    uint64_t top = spk::wave_max_u64(mx);
-    if (lane == 0) sh.part2[wv] = top;
-    const uint64_t total = block_sum<WAVES>(sh, c32);
-#pragma unroll
-    for (int q = 0; q < WAVES; ++q) top = sh.part2[q] > top ? sh.part2[q] : top;
-    if (top == 0) {  // nothing can win (uniform)
+    __shared__ RowSums sums[SPLITS * WAVES];
+    const int64_t b = blockIdx.x;
+    const int tid = threadIdx.x;
+    const RowEdge re = w.edge[b];
+    if (!re.any) {  // nothing can win (uniform)
         if (tid < 4) winners[b * 4 + tid] = -1;
         if (tid == 0) n_win[b] = 0;
         return;
     }
-    const Weigher weigh = weigher<WAVES>(sh, a, (uint32_t)top);
-    const float ftop = value_of((uint32_t)top), steps = a.temperature > 0.0f ? 64.0f / a.temperature : 1.0f;
-    auto bin_of = [&](uint32_t k) -> int {  // does not fall as the score falls
-        return k == (uint32_t)top ? 0 : (int)fminf((ftop - value_of(k)) * steps, (float)(BINS - 1));
-    };
+    const RowStat st(w.part + b * w.splits, w.splits, a.temperature);
+    const Weigher weigh = weigher<WAVES>(sh, a, key_of(st.top));
+    const int ns = w.splits * WAVES;
+    if (tid < ns) sums[tid] = w.sums[b * ns + tid];
+    __syncthreads();
     Edge e;
-    // moves the boundary to where the running total of value() reaches `want`; returns the new
-    // key and, in *above, the total of the larger ones
-    auto narrow = [&](uint64_t want, auto value, uint64_t *above) -> uint32_t {
-        const uint32_t from = e.edge;
-        for (int i = tid; i < BINS; i += LONG_THREADS) sh.hist[i] = 0;
-        if (tid == 0) sh.n_list = 0;
-        __syncthreads();
-        each([&](uint32_t k, int64_t) {
-            if (k >= from) {
-                const uint64_t v = value(k);
-                if (v) atomicAdd((unsigned long long *)&sh.hist[bin_of(k)], (unsigned long long)v);
-            }
-        });
-        uint64_t over, in;
-        const int bin = (int)find_bin<WAVES>(sh, BINS, want, &over);
-        each([&](uint32_t k, int64_t) {
-            if (k >= from && bin_of(k) == bin) {
-                const uint32_t at = atomicAdd(&sh.n_list, 1u);
-                if (at < LIST) sh.list[at] = k;
-            }
-        });
-        __syncthreads();
-        const uint32_t n = sh.n_list;
-        uint32_t key;
-        if (n <= LIST)
-            key = descend<WAVES>(sh, want - over, [&](auto f) {
-                for (uint32_t i = tid; i < n; i += LONG_THREADS) {
-                    const uint32_t k = sh.list[i];
-                    f(k, [&] { return value(k); });
-                }
-            }, &in);
-        else
-            key = descend<WAVES>(sh, want - over, [&](auto f) {
-                each([&](uint32_t k, int64_t) {
-                    if (k >= from && bin_of(k) == bin) f(k, [&] { return value(k); });
-                });
-            }, &in);
-        *above = over + in;
-        return key;
-    };
-    uint64_t above;
-    const uint64_t top_k = a.temperature > 0.0f ? (uint64_t)a.top_k : 1ull;
-    if (top_k == 1) {
-        e.edge = (uint32_t)top;
-        e.equal = 1;
-    } else if (top_k > 0 && top_k < total) {
-        const uint32_t k = narrow(top_k, [](uint32_t) -> uint64_t { return 1; }, &above);
-        e.edge = k;
-        e.equal = top_k - above;
-    }
-    __syncthreads();
-    if (a.top_p < 1.0f && top_k != 1) {
-        uint64_t sum = 0;
-        each([&](uint32_t k, int64_t) {
-            if (k > e.edge || (k == e.edge && e.equal == ~0ull)) sum += weigh(k);
-        });
-        sum = block_sum<WAVES>(sh, sum);
-        if (e.equal != ~0ull) sum += e.equal * weigh(e.edge);
-        const uint64_t want = share(a.top_p, sum);
-        const uint32_t k = narrow(want, weigh, &above);
-        e.by_weight(k, want, above, weigh(k));
-    }
+    e.edge = re.edge;
+    e.equal = re.equal;
     const uint64_t min_w = (uint64_t)ceil(ldexp((double)a.min_p, a.shift));
-    uint64_t we = weigh(e.edge);
+    uint64_t we = e.edge > 1 ? weigh(e.edge) : 0;
     we = we >= min_w ? we : 0;
-    // sums of the waves' segments of the row, and the segment of the draw
-    const int64_t seg = ((N + WAVES - 1) / WAVES + 63) / 64 * 64;
-    uint64_t sum = 0, eqs = 0;
-    for_row<E>(x, tf, a.T, min(N, wv * seg), min(N, (wv + 1) * seg), lane, 64, [&](uint32_t k, int64_t) {
-        const uint64_t w = k > e.edge ? weigh(k) : 0;
-        sum += w >= min_w ? w : 0;
-        eqs += k == e.edge;
-    });
-    sum = wave_sum_u64(sum);
-    eqs = wave_sum_u64(eqs);
-    __syncthreads();
-    if (lane == 0) {
-        sh.part[wv] = sum;
-        sh.part2[wv] = eqs;
+    // kept weight and equal keys before each segment (a thread a segment)
+    const RowSums own = tid < ns ? sums[tid] : RowSums{0, 0};
+    const int lane = tid & 63, wv = tid >> 6;
+    const uint64_t si = wave_scan_u64(own.kept, lane), ei = wave_scan_u64(own.equal, lane);
+    if (lane == 63) {
+        sh.part[wv] = si;
+        sh.part2[wv] = ei;
     }
     __syncthreads();
-    uint64_t left = e.equal, all = 0;
+    uint64_t run = si - own.kept, eq = ei - own.equal, all = 0, eq_all = 0;
     for (int q = 0; q < WAVES; ++q) {
-        const uint64_t m = sh.part2[q] < left ? sh.part2[q] : left;
-        left -= m;
-        all += sh.part[q] + m * we;
+        run += q < wv ? sh.part[q] : 0;
+        eq += q < wv ? sh.part2[q] : 0;
+        all += sh.part[q];
+        eq_all += sh.part2[q];
     }
-    const uint64_t target = target_of(u[b], all);
-    uint64_t run = 0, eq = 0;
-    int at_seg = 0;
-    for (int q = 0; q < WAVES; ++q) {
-        const uint64_t used = eq < e.equal ? eq : e.equal;
-        const uint64_t m = sh.part2[q] < e.equal - used ? sh.part2[q] : e.equal - used;
-        if (target < run + used * we + sh.part[q] + m * we) {
-            at_seg = q;
-            break;
-        }
-        run += sh.part[q];
-        eq += sh.part2[q];
+    const uint64_t target = target_of(u[b], all + (eq_all < e.equal ? eq_all : e.equal) * we);
+    const uint64_t used = eq < e.equal ? eq : e.equal, left = e.equal - used;
+    const uint64_t before = run + used * we, mine = own.kept + (own.equal < left ? own.equal : left) * we;
+    if (target >= before && target < before + mine) {
+        sh.bin = (uint32_t)tid;
+        sh.above = run;
+        sh.hist[0] = eq;
     }
-    const int64_t g0 = min(N, at_seg * seg), g1 = min(N, g0 + seg), per = (g1 - g0 + LONG_THREADS - 1) / LONG_THREADS;
+    __syncthreads();
+    const int at_seg = (int)sh.bin;
+    run = sh.above;
+    eq = sh.hist[0];
+    const LongRow<E> row(scores, t_first, a, w.splits, b, at_seg / WAVES);
+    const int64_t g0 = min(row.i1, row.i0 + (at_seg % WAVES) * row.seg), g1 = min(row.i1, g0 + row.seg);
+    const int64_t per = (g1 - g0 + LONG_THREADS - 1) / LONG_THREADS;
     const int64_t i0 = min(g1, g0 + tid * per), i1 = min(g1, i0 + per);
     int64_t at;
     if (pick<WAVES>(sh, we, e, min_w, target, run, eq, i1 - i0, [&](int64_t i) {
-            const uint32_t k = key_of(as_float<E>(x[i0 + i]));
-            return tf && tf[i0 + i] >= a.T ? 0u : k;
+            const uint32_t k = key_of(as_float<E>(row.x[i0 + i]));
+            return row.tf && row.tf[i0 + i] >= a.T ? 0u : k;
         }, [&](int64_t, uint32_t k) { return weigh(k); }, &at))
-        put_winner(winners, n_win, b, i0 + at, tf ? (int)tf[i0 + at] : 0, a);
+        put_winner(winners, n_win, b, i0 + at, row.tf ? (int)row.tf[i0 + at] : 0, a);
+}
+
+constexpr int64_t SHORT_MAX = 16 * 64 * 16;  // keys of a row that the registers of a workgroup take
+
+// Workgroups of a long row: about two for each of 256 CUs in all, no less than
+// 4096 scores each.
+int splits_of(int B, int64_t N) {
+    int64_t s = 512 / B;
+    s = s < N / 4096 ? s : N / 4096;
+    return (int)(s < 1 ? 1 : s > SPLITS ? SPLITS : s);
+}
+
+size_t carve(void *ws, int B, int64_t N, Work *w) {
+    spk::Carver c(ws);
+    w->splits = splits_of(B, N);
+    w->hist = c.take<uint64_t>((size_t)B * BINS);
+    w->list = c.take<uint32_t>((size_t)B * LIST);
+    w->count = c.take<uint32_t>(B);
+    w->part = c.take<RowPart>((size_t)B * w->splits);
+    w->sums = c.take<RowSums>((size_t)B * w->splits * LONG_WAVES);
+    w->edge = c.take<RowEdge>(B);
+    return spk::align_up(c.off, 256);
 }
 
 template <class E>
 void launch(const void *scores, const uint8_t *t_first, const float *u, int B, const SampleArgs &a, int32_t *winners,
-            int32_t *n_winners, hipStream_t st) {
+            int32_t *n_winners, void *ws, hipStream_t st) {
     const E *x = static_cast<const E *>(scores);
-    const dim3 grid((unsigned)B);
-    if (a.N <= 4 * 64 * 16)
-        hipLaunchKernelGGL((k_sample_short<E, 4>), grid, dim3(256), 0, st, x, t_first, u, a, winners, n_winners);
-    else if (a.N <= 16 * 64 * 16)
-        hipLaunchKernelGGL((k_sample_short<E, 16>), grid, dim3(1024), 0, st, x, t_first, u, a, winners, n_winners);
-    else
-        hipLaunchKernelGGL(k_sample_long<E>, grid, dim3(LONG_THREADS), 0, st, x, t_first, u, a, winners, n_winners);
+    const dim3 rows((unsigned)B), threads(LONG_THREADS);
+    if (a.N <= 4 * 64 * 16) {
+        hipLaunchKernelGGL((k_sample_short<E, 4>), rows, dim3(256), 0, st, x, t_first, u, a, winners, n_winners);
+        return;
+    }
+    if (a.N <= SHORT_MAX) {
+        hipLaunchKernelGGL((k_sample_short<E, 16>), rows, threads, 0, st, x, t_first, u, a, winners, n_winners);
+        return;
+    }
+    Work w;
+    carve(ws, B, a.N, &w);
+    const dim3 grid((unsigned)w.splits, (unsigned)B);
+    hipLaunchKernelGGL(k_sample_top<E>, grid, threads, 0, st, x, t_first, a, w);
+    const bool one = a.temperature == 0.0f || a.top_k == 1, by_count = !one && a.top_k > 0 && a.top_k < a.N;
+    if (by_count) {
+        hipLaunchKernelGGL((k_sample_hist<E, true>), grid, threads, 0, st, x, t_first, a, w);
+        hipLaunchKernelGGL((k_sample_list<E, true>), grid, threads, 0, st, x, t_first, a, w);
+        hipLaunchKernelGGL((k_sample_sums<E, 2>), grid, threads, 0, st, x, t_first, a, w);
+    } else if (!one && a.top_p < 1.0f) {
+        hipLaunchKernelGGL((k_sample_hist<E, false>), grid, threads, 0, st, x, t_first, a, w);
+        hipLaunchKernelGGL((k_sample_list<E, false>), grid, threads, 0, st, x, t_first, a, w);
+        hipLaunchKernelGGL((k_sample_sums<E, 1>), grid, threads, 0, st, x, t_first, a, w);
+    } else {
+        hipLaunchKernelGGL((k_sample_sums<E, 0>), grid, threads, 0, st, x, t_first, a, w);
+    }
+    hipLaunchKernelGGL(k_sample_pick<E>, rows, threads, 0, st, x, t_first, u, a, w, winners, n_winners);
+}
+
+int check(int dtype, int B, int C, int H, int W, const char *name) {
+    SPK_REQUIRE(dtype == SPK_F32 || dtype == SPK_BF16, SPK_E_ARG, "%s: dtype %d is neither SPK_F32 nor SPK_BF16", name,
+                dtype);
+    SPK_REQUIRE(B >= 0 && C >= 1 && H >= 1 && W >= 1, SPK_E_SHAPE, "%s: bad sizes", name);
+    SPK_REQUIRE((int64_t)C * H <= (1 << 24) && (int64_t)C * H * W <= (1 << 24), SPK_E_RANGE, "%s: C*H*W above 2^24",
+                name);
+    // (a workgroup an image, of up to 1024 threads; long rows have a grid dimension for the images)
+    SPK_REQUIRE(B <= (1 << 21) && ((int64_t)C * H * W <= SHORT_MAX || B <= 65535), SPK_E_RANGE,
+                "%s: B=%d above 2^21, or above 65535 with C*H*W above 16384", name, B);
+    return SPK_OK;
 }
 
 }  // namespace
 
 extern "C" size_t spk_sample_winners_workspace_size(int dtype, int B, int C, int H, int W) {
-    (void)dtype, (void)B, (void)C, (void)H, (void)W;
-    return 0;
+    if (check(dtype, B, C, H, W, "") != SPK_OK || B == 0) return 0;
+    const int64_t N = (int64_t)C * H * W;
+    Work w;
+    return N > SHORT_MAX ? carve(nullptr, B, N, &w) : 0;
 }
 
 extern "C" int spk_sample_winners(const void *scores, int dtype, const uint8_t *t_first, const float *u, int B, int T,
@@ -601,13 +824,9 @@ extern "C" int spk_sample_winners(const void *scores, int dtype, const uint8_t *
                                   int32_t *winners, int32_t *n_winners, void *workspace, size_t ws_bytes,
                                   void *stream) {
     const char *name = "spk_sample_winners";
-    SPK_REQUIRE(dtype == SPK_F32 || dtype == SPK_BF16, SPK_E_ARG, "%s: dtype %d is neither SPK_F32 nor SPK_BF16", name,
-                dtype);
-    SPK_REQUIRE(B >= 0 && C >= 1 && H >= 1 && W >= 1 && T >= 1, SPK_E_SHAPE, "%s: bad sizes", name);
+    if (int rc = check(dtype, B, C, H, W, name)) return rc;
+    SPK_REQUIRE(T >= 1, SPK_E_SHAPE, "%s: bad sizes", name);
     SPK_REQUIRE(T <= 255, SPK_E_RANGE, "%s: T=%d > 255", name, T);
-    SPK_REQUIRE((int64_t)C * H <= (1 << 24) && (int64_t)C * H * W <= (1 << 24), SPK_E_RANGE, "%s: C*H*W above 2^24",
-                name);
-    SPK_REQUIRE(B <= (1 << 21), SPK_E_RANGE, "%s: B=%d > 2^21", name, B);
     SPK_REQUIRE(temperature >= 0.0f && std::isfinite(temperature), SPK_E_ARG, "%s: temperature must be finite and >= 0",
                 name);
     SPK_REQUIRE(top_k >= 0, SPK_E_ARG, "%s: top_k=%d < 0", name, top_k);
@@ -616,7 +835,9 @@ extern "C" int spk_sample_winners(const void *scores, int dtype, const uint8_t *
     if (B == 0) return spk::ok();
     SPK_REQUIRE(scores && u && winners && n_winners, SPK_E_ARG, "%s: scores, u, winners and n_winners are required",
                 name);
-    (void)workspace, (void)ws_bytes;
+    const size_t need = spk_sample_winners_workspace_size(dtype, B, C, H, W);
+    SPK_REQUIRE(need == 0 || (workspace && ws_bytes >= need), SPK_E_WORKSPACE, "%s: workspace of %zu bytes, %zu needed",
+                name, workspace ? ws_bytes : (size_t)0, need);
     SampleArgs a;
     a.N = (int64_t)C * H * W;
     a.T = T;
@@ -630,7 +851,7 @@ extern "C" int spk_sample_winners(const void *scores, int dtype, const uint8_t *
     while ((1ll << lg) < a.N) ++lg;
     a.shift = 62 - lg;
     hipStream_t st = spk::as_stream(stream);
-    if (dtype == SPK_F32) launch<float>(scores, t_first, u, B, a, winners, n_winners, st);
-    else launch<uint16_t>(scores, t_first, u, B, a, winners, n_winners, st);
+    if (dtype == SPK_F32) launch<float>(scores, t_first, u, B, a, winners, n_winners, workspace, st);
+    else launch<uint16_t>(scores, t_first, u, B, a, winners, n_winners, workspace, st);
     return spk::check_launch(name);
 }

@@ -241,6 +241,63 @@ def test_sample_of_long_rows():
             assert torch.equal(w[:, 0, 0].cpu().long(), at) and bool((n == 1).all())
 
 
+def in_order(x, u, temperature, top_k, top_p, min_p):
+    """The definition on whole rows at once (x f64 [B,N], -inf = cannot win), in 64 bits."""
+    v, order = x.sort(dim=1, descending=True, stable=True)
+    e = torch.where(v == v[:, :1], 1.0, torch.exp((v - v[:, :1]) / temperature))
+    e[:, top_k or x.shape[1]:] = 0
+    c = e.cumsum(1)
+    e = torch.where((c - e < top_p * c[:, -1:]) & (e >= min_p), e, 0.0)
+    e = torch.zeros_like(e).scatter_(1, order, e)
+    c = e.cumsum(1)
+    return (c <= u.double()[:, None] * c[:, -1:]).sum(1)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("B,C,H,W", [(3, 50001, 1, 1), (2, 333, 9, 17), (700, 16385, 1, 1)])
+def test_sample_of_long_masked_rows(B, C, H, W, dtype):
+    """Rows of several workgroups, of odd lengths (so that every row starts at another alignment), with silent
+    neurons; scores of few steps, so that a boundary's bin holds more equal ones than LDS takes."""
+    randn, rand = seeded(B)
+    N = C * H * W
+    fine = (randn(B, C, H, W) * 3).to(dtype)
+    for x in (fine, (fine.float() * 2).round().to(dtype) / 2):
+        u = rand(B)
+        tf = torch.where(rand(B, C, H, W) < 0.5, 6, 7).to(torch.uint8)
+        tf[0] = 7
+        flat = torch.where(tf < 7, x.double(), -math.inf).reshape(B, N)
+        some = flat.max(1).values > -math.inf
+        for kw in (dict(top_p=0.75), dict(temperature=5.0, top_p=0.5, min_p=0.25), dict(top_k=40), dict(),
+                   dict(top_k=9000, top_p=0.9375), dict(temperature=0.5, top_k=60, top_p=0.5, min_p=0.125),
+                   dict(top_k=N - 1, top_p=0.875)):
+            w, n = spk.spk_sample_winners(x.cuda(), u.cuda(), t_first=tf.cuda(), T=7, **kw)
+            at = in_order(flat.cuda(), u.cuda(), **{"temperature": 1.0, "top_k": 0, "top_p": 1.0, "min_p": 0.0, **kw})
+            at = at.clamp(max=N - 1).cpu()
+            want = torch.stack([at // (H * W), torch.full_like(at, 6), at // W % H, at % W], 1)
+            want = torch.where(some[:, None], want, -1)
+            assert torch.equal(w[:, 0].cpu().long(), want) and torch.equal(n.cpu().bool(), some), kw
+
+
+def test_sample_of_long_rows_at_the_ends():
+    """All equal, all masked, infinities, the type's lowest value, greedy; u at its ends."""
+    N = 40000
+    x = torch.zeros(8, N, 1, 1)
+    x[1] = -math.inf
+    x[2] = math.nan
+    x[3, 7:9] = math.inf
+    x[4] = torch.finfo(F32).min
+    x[5, 1:] = torch.finfo(F32).min
+    x[6] = -0.0
+    x[6, 20000:] = 0.0
+    x[7, ::2] = -1e30
+    u = torch.tensor([1.0 - 2.0 ** -24, 0.5, 0.5, 0.75, 0.5, 0.999, 1.0, math.nan])
+    first = lambda kw: spk.spk_sample_winners(x.cuda(), u.cuda(), **kw)[0][:, 0, 0].tolist()  # noqa: E731
+    assert first(dict()) == [N - 1, -1, -1, 8, N // 2, 0, N - 1, 1]
+    assert first(dict(temperature=0.0)) == [0, -1, -1, 7, 0, 0, 0, 1]
+    assert first(dict(top_k=2)) == [1, -1, -1, 8, 1, 0, 1, 1]
+    assert first(dict(top_p=0.5)) == [N // 2 - 1, -1, -1, 7, N // 4, 0, N // 2 - 1, 1]
+
+
 # ---------------------------------------------------------------- together
 def test_readout_learns_draws_and_rewards():
     """As a program uses them: a layer's potentials as features, a readout learnt over the images in order,
