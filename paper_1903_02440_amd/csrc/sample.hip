@@ -13,6 +13,7 @@
 // boundary's bin; sums by index; the draw), each reading the row again: a step is
 // bound by reading the row, and where it weighs scores by some 30 instructions for
 // each, half of them in double precision.
+#include <algorithm>
 #include <cmath>
 
 #include "common.hpp"
@@ -58,35 +59,33 @@ __device__ __forceinline__ uint64_t wave_scan_u64(uint64_t v, int lane) {  // in
     return v;
 }
 
-constexpr int POW = 128;    // entries of the table of 2^(j / POW)
+constexpr int POW_BITS = 7, POW = 1 << POW_BITS;  // entries of the table of 2^(j / POW)
 constexpr int BINS = 2048;  // bins of a row's first histogram
 constexpr int LIST = 4096;  // keys of one bin that LDS takes
 
-// Weights of a row: floor(2^shift exp((score - largest) / temperature)).  With
-// y = shift + (score - largest) log2(e) / temperature = n + j / POW + r, it is
-// 2^n 2^(j / POW) 2^r with 2^r from its series: the last term left out,
-// (r ln 2)^6 / 720, is below 4e-17.  The largest itself (also +inf) weighs 2^shift.
+// Weights of a row: 2^shift exp((score - largest) / temperature), to the nearest
+// integer.  With y = shift + (score - largest) log2(e) / temperature rounded to
+// n + j / POW (by adding a number whose last place that is) and r what rounding
+// left, it is 2^n 2^(j / POW) 2^r with 2^r from its series: the first term left
+// out, (r ln 2)^5 / 120, is below 2e-15.  +infinity as the largest weighs 2^shift.
 struct Weigher {
     double top, per, shift_d;
-    int shift;
+    float ftop;
     const double *pow;
     __device__ __forceinline__ uint64_t operator()(uint32_t k) const { return of(value_of(k)); }
     __device__ __forceinline__ uint64_t of(float v) const {
-        const double y = fmax(fma((double)v - top, per, shift_d), -1.0);
-        const double n = floor(y), f = y - n;
-        const int j = (int)(f * POW);
-        const double t = (f - j * (1.0 / POW)) * 0.69314718055994530942;
-        double p = fma(t, 1.0 / 120, 1.0 / 24);
-        p = fma(t, p, 1.0 / 6);
-        p = fma(t, p, 0.5);
-        p = fma(t, p, 1.0);
-        p = fma(t, p, 1.0);
-        const uint64_t bits = __double_as_longlong(pow[j & (POW - 1)] * p);  // in [1, 2]
-        // the significand as an integer times 2^(n - 52), and 2^n a bit on where rounding reached 2
-        const int e = (int)n + (int)(bits >> 52) - 1023 - 52;
-        const uint64_t sig = (bits & 0xFFFFFFFFFFFFFull) | 0x10000000000000ull;
-        const uint64_t w = e >= 0 ? sig << e : sig >> -e;
-        return (double)v == top ? 1ull << shift : y >= 0.0 ? w : 0ull;
+        constexpr double LN2 = 0.69314718055994530942, STEP = 6755399441055744.0 / POW;  // 1.5 * 2^52 / POW
+        const double d = v == ftop ? 0.0 : (double)v - top;
+        const double y = fmax(fma(d, per, shift_d), -2.0);  // (below half: weight 0; NaN too)
+        const double z = y + STEP;
+        const int nj = (int)(uint32_t)__double_as_longlong(z);
+        const double r = y - (z - STEP);
+        double p = fma(r, LN2 * LN2 * LN2 * LN2 / 24, LN2 * LN2 * LN2 / 6);
+        p = fma(r, p, LN2 * LN2 / 2);
+        p = fma(r, p, LN2);
+        p = fma(r, p, 1.0);
+        const double w = ldexp(pow[nj & (POW - 1)] * p, nj >> POW_BITS);
+        return (uint64_t)__double_as_longlong(w + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;  // (w < 2^52)
     }
 };
 
@@ -202,7 +201,7 @@ __device__ __forceinline__ Weigher weigher(Shared<WAVES> &sh, const SampleArgs &
     Weigher w;
     w.top = (double)value_of(ktop);
     w.per = a.temperature > 0.0f ? 1.4426950408889634074 / (double)a.temperature : 0.0;
-    w.shift = a.shift;
+    w.ftop = value_of(ktop);
     w.shift_d = (double)a.shift;
     w.pow = sh.pow;
     return w;
@@ -273,7 +272,7 @@ __device__ __forceinline__ bool pick(Shared<WAVES> &sh, uint64_t we, const Edge 
 // Grid: one workgroup per image, whose row of at most 16 keys a thread stays in
 // registers; a thread's keys follow each other in index.
 template <class E, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void k_sample_short(const E *__restrict__ scores,
+__global__ __launch_bounds__(WAVES * 64, 4) void k_sample_short(const E *__restrict__ scores,
                                                              const uint8_t *__restrict__ t_first,
                                                              const float *__restrict__ u, SampleArgs a,
                                                              int32_t *__restrict__ winners,
@@ -573,14 +572,22 @@ __global__ __launch_bounds__(LONG_THREADS) void k_sample_list(const E *__restric
     uint64_t want, over;
     const int bin = boundary_bin<COUNT>(sh, a, w, b, &want, &over);
     const LongRow<E> row(scores, t_first, a, w.splits, b, blockIdx.x);
+    if (threadIdx.x == 0) sh.n_list = 0;
+    __syncthreads();
     row.own([&](float v, int64_t) {
         if (!wins(v)) return;
         const int at_bin = st.bin(v);
         if (at_bin == bin || (COUNT && at_bin < bin)) {
-            const uint32_t at = atomicAdd(&w.count[b], 1u);
-            if (at < LIST) w.list[b * LIST + at] = key_of(v);
+            const uint32_t at = atomicAdd(&sh.n_list, 1u);
+            if (at < LIST) sh.list[at] = key_of(v);
         }
     });
+    __syncthreads();
+    const uint32_t n = sh.n_list;  // (beyond LIST the row goes without its list)
+    if (threadIdx.x == 0) sh.bin = n ? atomicAdd(&w.count[b], n) : 0;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x, at = sh.bin; i < n && i < LIST; i += LONG_THREADS)
+        if (at + i < LIST) w.list[b * LIST + at + i] = sh.list[i];
 }
 
 // The boundary (each workgroup of the row finds it for itself), then the sums of
@@ -849,7 +856,7 @@ extern "C" int spk_sample_winners(const void *scores, int dtype, const uint8_t *
     a.min_p = min_p;
     int lg = 0;
     while ((1ll << lg) < a.N) ++lg;
-    a.shift = 62 - lg;
+    a.shift = std::min(51, 62 - lg);
     hipStream_t st = spk::as_stream(stream);
     if (dtype == SPK_F32) launch<float>(scores, t_first, u, B, a, winners, n_winners, workspace, st);
     else launch<uint16_t>(scores, t_first, u, B, a, winners, n_winners, workspace, st);
