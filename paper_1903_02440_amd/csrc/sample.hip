@@ -113,28 +113,68 @@ __device__ __forceinline__ uint64_t block_sum(Shared<WAVES> &sh, uint64_t v) {
     return s;
 }
 
-// The first of n bins (from bin 0) at which the running total reaches `want`,
+// The first of N bins (from bin 0) at which the running total reaches `want`,
 // the last one if it never does; *above gets the total of the bins before it.
-template <int WAVES>
-__device__ __forceinline__ uint32_t find_bin(Shared<WAVES> &sh, int n, uint64_t want, uint64_t *above) {
+template <int N, int WAVES>
+__device__ __forceinline__ uint32_t find_bin(Shared<WAVES> &sh, uint64_t want, uint64_t *above) {
     __syncthreads();
     if (threadIdx.x < 64) {
-        const int lane = threadIdx.x, per = n / 64;
-        uint64_t sum = 0;
-        for (int j = 0; j < per; ++j) sum += sh.hist[lane * per + j];
+        constexpr int PER = N / 64;
+        const int lane = threadIdx.x;
+        uint64_t v[PER], sum = 0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) v[j] = sh.hist[lane * PER + j];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) sum += v[j];
         const uint64_t incl = wave_scan_u64(sum, lane);
         const uint64_t hit = __ballot(incl >= want);
         const int src = hit ? __ffsll((unsigned long long)hit) - 1 : 63;
+        uint64_t run = incl - sum;
+        int at = PER - 1;
+        bool found = false;
+#pragma unroll
+        for (int j = 0; j < PER - 1; ++j) {
+            if (!found && run + v[j] >= want) {
+                at = j;
+                found = true;
+            }
+            run += found ? 0 : v[j];
+        }
         if (lane == src) {
-            uint64_t run = incl - sum;
-            int j = 0;
-            for (; j < per - 1 && run + sh.hist[lane * per + j] < want; ++j) run += sh.hist[lane * per + j];
-            sh.bin = (uint32_t)(lane * per + j);
+            sh.bin = (uint32_t)(lane * PER + at);
             sh.above = run;
         }
     }
     __syncthreads();
     *above = sh.above;
+    return sh.bin;
+}
+
+// The key at which the running total of value(k), from the largest key, reaches
+// `want` among the n <= 64 keys of the list that are not below `from`: a key a
+// lane, each against all.  *above_edge gets the total of the larger keys.
+template <int WAVES, class Value>
+__device__ __forceinline__ uint32_t few(Shared<WAVES> &sh, uint32_t n, uint32_t from, uint64_t want, Value value,
+                                        uint64_t *above_edge) {
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        const uint32_t x = threadIdx.x < n ? sh.list[threadIdx.x] : 0, k = x >= from ? x : 0;
+        const uint64_t v = k ? value(k) : 0;
+        uint64_t above = 0, equal = 0;
+        for (uint32_t j = 0; j < n; ++j) {
+            const uint32_t kj = (uint32_t)__builtin_amdgcn_readlane((int)k, (int)j);
+            const uint64_t vj = ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), (int)j) << 32) |
+                                (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, (int)j);
+            above += kj > k ? vj : 0;
+            equal += kj == k ? vj : 0;
+        }
+        if (k && above < want && want <= above + equal) {  // (equal keys write the same)
+            sh.bin = k;
+            sh.above = above;
+        }
+    }
+    __syncthreads();
+    *above_edge = sh.above;
     return sh.bin;
 }
 
@@ -156,7 +196,7 @@ __device__ __forceinline__ uint32_t descend(Shared<WAVES> &sh, uint64_t want, Ea
             }
         });
         uint64_t over;
-        const uint32_t bin = find_bin<WAVES>(sh, 256, want - above, &over);
+        const uint32_t bin = find_bin<256, WAVES>(sh, want - above, &over);
         prefix = (prefix << 8) | (255 - bin);
         above += over;
     }
@@ -207,17 +247,35 @@ __device__ __forceinline__ Weigher weigher(Shared<WAVES> &sh, const SampleArgs &
     return w;
 }
 
+// Sums over the threads before this one, and over all.
+template <int WAVES>
+__device__ __forceinline__ void before_and_all(Shared<WAVES> &sh, uint64_t x, uint64_t y, uint64_t *xb, uint64_t *yb,
+                                               uint64_t *xa, uint64_t *ya) {
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    const uint64_t xi = wave_scan_u64(x, lane), yi = wave_scan_u64(y, lane);
+    __syncthreads();
+    if (lane == 63) {
+        sh.part[wv] = xi;
+        sh.part2[wv] = yi;
+    }
+    __syncthreads();
+    *xb = xi - x, *yb = yi - y, *xa = 0, *ya = 0;
+    for (int q = 0; q < WAVES; ++q) {
+        *xb += q < wv ? sh.part[q] : 0;
+        *yb += q < wv ? sh.part2[q] : 0;
+        *xa += sh.part[q];
+        *ya += sh.part2[q];
+    }
+}
+
 // The draw among `n` keys of a thread that follow each other in index (0 =
 // cannot win): keys above the edge and the first `equal` equal to it, of weight
-// min_w at least.  key_at(i) gives the thread's i-th key, weight_at(i, key) its
-// weight.  `run`, `eq`: kept weight and equal keys before the workgroup's first.
+// min_w at least.  key_at(i) gives the thread's i-th key.  `run`, `eq`: kept weight and equal keys before the workgroup's first.
 // Returns whether this thread holds the winner, and its number.
-template <int WAVES, class KeyAt, class WeightAt>
-__device__ __forceinline__ bool pick(Shared<WAVES> &sh, uint64_t we, const Edge &e, uint64_t min_w, uint64_t target,
-                                     uint64_t run, uint64_t eq, int64_t n, KeyAt key_at, WeightAt weight_at,
-                                     int64_t *at) {
+template <int WAVES, class KeyAt>
+__device__ __forceinline__ bool pick(Shared<WAVES> &sh, const Weigher &weigh, uint64_t we, const Edge &e, uint64_t min_w, uint64_t target,
+                                     uint64_t run, uint64_t eq, int64_t n, KeyAt key_at, int64_t *at) {
     constexpr int AHEAD = 8;  // keys read at a time
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
     uint64_t sum = 0, eqs = 0;
     for (int64_t i = 0; i < n; i += AHEAD) {
         uint32_t k[AHEAD];
@@ -226,24 +284,15 @@ __device__ __forceinline__ bool pick(Shared<WAVES> &sh, uint64_t we, const Edge 
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
             if (i + j >= n) continue;
-            const uint64_t w = k[j] > e.edge ? weight_at(i + j, k[j]) : 0;
+            const uint64_t w = k[j] > e.edge ? weigh(k[j]) : 0;
             sum += w >= min_w ? w : 0;
             eqs += k[j] == e.edge;
         }
     }
-    const uint64_t si = wave_scan_u64(sum, lane), ei = wave_scan_u64(eqs, lane);
-    __syncthreads();
-    if (lane == 63) {
-        sh.part[wv] = si;
-        sh.part2[wv] = ei;
-    }
-    __syncthreads();
-    for (int q = 0; q < wv; ++q) {
-        run += sh.part[q];
-        eq += sh.part2[q];
-    }
-    run += si - sum;
-    eq += ei - eqs;
+    uint64_t run_in, eq_in, all, eq_all;
+    before_and_all<WAVES>(sh, sum, eqs, &run_in, &eq_in, &all, &eq_all);
+    run += run_in;
+    eq += eq_in;
     // kept weight before this thread, equal keys among it
     const uint64_t before = run + (eq < e.equal ? eq : e.equal) * we;
     const uint64_t left = eq < e.equal ? e.equal - eq : 0;
@@ -254,7 +303,7 @@ __device__ __forceinline__ bool pick(Shared<WAVES> &sh, uint64_t we, const Edge 
         const uint32_t k = key_at(i);
         uint64_t w = 0;
         if (k > e.edge) {
-            w = weight_at(i, k);
+            w = weigh(k);
             w = w >= min_w ? w : 0;
         } else if (k == e.edge && l) {
             w = we;
@@ -267,6 +316,51 @@ __device__ __forceinline__ bool pick(Shared<WAVES> &sh, uint64_t we, const Edge 
         }
     }
     return false;  // (not reached)
+}
+
+// Bins of a row's histogram: equal steps of the score from the largest down to
+// the smallest, or to where weights end (44 temperatures); the last bin takes the rest.
+struct Bins {
+    float top, steps, last;
+    __device__ __forceinline__ Bins(float hi, float lo, float temperature, int n)
+        : top(hi), steps((float)(n - 2) / fmaxf(fminf(hi - lo, 44.0f * temperature), 1e-30f)), last((float)(n - 1)) {}
+    __device__ __forceinline__ int operator()(float v) const {  // does not fall as the score falls
+        return v == top ? 0 : (int)fminf((top - v) * steps, last);
+    }
+};
+
+constexpr int SHORT_BINS = 512;  // of a short row
+
+// As descend(), by a histogram of SHORT_BINS bins first and then the boundary's
+// bin alone, whose keys are few as a rule.
+template <int WAVES, class Each, class Value>
+__device__ __forceinline__ uint32_t boundary(Shared<WAVES> &sh, const Bins &bins, uint32_t from, uint64_t want, Each each,
+                                             Value value, uint64_t *above_edge) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < SHORT_BINS; i += WAVES * 64) sh.hist[i] = 0;
+    if (threadIdx.x == 0) sh.n_list = 0;
+    __syncthreads();
+    each([&](uint32_t k, auto v) {
+        atomicAdd((unsigned long long *)&sh.hist[bins(value_of(k))], (unsigned long long)v());
+    });
+    uint64_t over, in;
+    const int bin = (int)find_bin<SHORT_BINS, WAVES>(sh, want, &over);
+    each([&](uint32_t k, auto) {
+        if (bins(value_of(k)) == bin) {
+            const uint32_t at = atomicAdd(&sh.n_list, 1u);
+            if (at < 64) sh.list[at] = k;
+        }
+    });
+    __syncthreads();
+    const uint32_t n = sh.n_list;
+    const uint32_t key = n <= 64 ? few<WAVES>(sh, n, from, want - over, value, &in)
+                                 : descend<WAVES>(sh, want - over, [&](auto f) {
+                                       each([&](uint32_t k, auto v) {
+                                           if (bins(value_of(k)) == bin) f(k, v);
+                                       });
+                                   }, &in);
+    *above_edge = over + in;
+    return key;
 }
 
 // Grid: one workgroup per image, whose row of at most 16 keys a thread stays in
@@ -298,37 +392,48 @@ __global__ __launch_bounds__(WAVES * 64, 4) void k_sample_short(const E *__restr
 #pragma unroll
         for (int j = 0; j < KEYS; ++j) key[j] = key_of(as_float<E>(raw[j]));
     }
-    uint64_t top = 0, cnt = 0;
+    uint32_t hi = 0, low = 0;  // largest and (of ~key) smallest key that can win
+    uint64_t cnt = 0;
 #pragma unroll
     for (int j = 0; j < KEYS; ++j) {
         key[j] = j < per && i0 + j < N ? key[j] : 0u;
-        top = key[j] > top ? key[j] : top;
+        hi = max(hi, key[j]);
+        low = max(low, key[j] ? ~key[j] : 0u);
         cnt += key[j] != 0;
     }
-    top = spk::wave_max_u64(top);
-    if ((tid & 63) == 0) sh.part2[tid >> 6] = top;
+#pragma unroll
+    for (int s = 32; s >= 1; s >>= 1) {
+        hi = max(hi, (uint32_t)__shfl_xor((int)hi, s, 64));
+        low = max(low, (uint32_t)__shfl_xor((int)low, s, 64));
+    }
+    if ((tid & 63) == 0) sh.part2[tid >> 6] = ((uint64_t)hi << 32) | low;
     const uint64_t total = block_sum<WAVES>(sh, cnt);
 #pragma unroll
-    for (int q = 0; q < WAVES; ++q) top = sh.part2[q] > top ? sh.part2[q] : top;
+    for (int q = 0; q < WAVES; ++q) {
+        hi = max(hi, (uint32_t)(sh.part2[q] >> 32));
+        low = max(low, (uint32_t)sh.part2[q]);
+    }
+    const uint32_t top = hi;
     if (top == 0) {  // nothing can win (uniform)
         if (tid < 4) winners[b * 4 + tid] = -1;
         if (tid == 0) n_win[b] = 0;
         return;
     }
-    const Weigher weigh = weigher<WAVES>(sh, a, (uint32_t)top);
+    const Weigher weigh = weigher<WAVES>(sh, a, top);
+    const Bins bins(value_of(top), value_of(~low), a.temperature, SHORT_BINS);
     __syncthreads();
     Edge e;
     uint64_t above;
     const uint64_t top_k = a.temperature > 0.0f ? (uint64_t)a.top_k : 1ull;
     if (top_k == 1) {
-        e.edge = (uint32_t)top;
+        e.edge = top;
         e.equal = 1;
     } else if (top_k > 0 && top_k < total) {
-        e.edge = descend<WAVES>(sh, top_k, [&](auto f) {
+        e.edge = boundary<WAVES>(sh, bins, 1, top_k, [&](auto f) {
 #pragma unroll
             for (int j = 0; j < KEYS; ++j)
                 if (key[j]) f(key[j], [] { return (uint64_t)1; });
-        }, &above);
+        }, [](uint32_t) { return (uint64_t)1; }, &above);
         e.equal = top_k - above;
     }
     uint64_t w[KEYS];
@@ -342,11 +447,11 @@ __global__ __launch_bounds__(WAVES * 64, 4) void k_sample_short(const E *__restr
         if (e.equal != ~0ull) sum += e.equal * weigh(e.edge);
         const uint64_t want = share(a.top_p, sum);
         // (the edge of step 1 takes part with all its equals: one that step 1 cut has its own limit)
-        const uint32_t k = descend<WAVES>(sh, want, [&](auto f) {
+        const uint32_t k = boundary<WAVES>(sh, bins, e.edge, want, [&](auto f) {
 #pragma unroll
             for (int j = 0; j < KEYS; ++j)
                 if (w[j]) f(key[j], [&] { return w[j]; });
-        }, &above);
+        }, weigh, &above);
         e.by_weight(k, want, above, weigh(k));
     }
     const uint64_t min_w = (uint64_t)ceil(ldexp((double)a.min_p, a.shift));
@@ -359,22 +464,22 @@ __global__ __launch_bounds__(WAVES * 64, 4) void k_sample_short(const E *__restr
         sum += w[j];
         eqs += key[j] == e.edge;
     }
-    sum = block_sum<WAVES>(sh, sum);
-    eqs = block_sum<WAVES>(sh, eqs);
-    const uint64_t target = target_of(u[b], sum + (eqs < e.equal ? eqs : e.equal) * we);
-    int64_t at;
-    if (pick<WAVES>(sh, we, e, min_w, target, 0, 0, per, [&](int64_t i) {
-            uint32_t k = 0;
+    uint64_t run, eq, all, eq_all;
+    before_and_all<WAVES>(sh, sum, eqs, &run, &eq, &all, &eq_all);
+    const uint64_t target = target_of(u[b], all + (eq_all < e.equal ? eq_all : e.equal) * we);
+    // the thread that holds the target walks its keys
+    uint64_t left = e.equal - (eq < e.equal ? eq : e.equal);
+    run += (eq < e.equal ? eq : e.equal) * we;
+    if (!(target >= run && target < run + sum + (eqs < left ? eqs : left) * we)) return;
+    int at = -1;
 #pragma unroll
-            for (int j = 0; j < KEYS; ++j) k = j == i ? key[j] : k;
-            return k;
-        }, [&](int64_t i, uint32_t) {
-            uint64_t x = 0;
-#pragma unroll
-            for (int j = 0; j < KEYS; ++j) x = j == i ? w[j] : x;
-            return x;
-        }, &at))
-        put_winner(winners, n_win, b, i0 + at, tf ? (int)tf[i0 + at] : 0, a);
+    for (int j = 0; j < KEYS; ++j) {
+        const bool is_edge = key[j] == e.edge && left > 0;
+        left -= is_edge;
+        run += w[j] + (is_edge ? we : 0);
+        at = at < 0 && run > target ? j : at;
+    }
+    put_winner(winners, n_win, b, i0 + at, tf ? (int)tf[i0 + at] : 0, a);
 }
 
 constexpr int LONG_WAVES = 16, LONG_THREADS = LONG_WAVES * 64;
@@ -466,28 +571,29 @@ struct LongRow {
     __device__ __forceinline__ void all(F f) const { for_row<E>(x, tf, T, 0, N, threadIdx.x, LONG_THREADS, f); }
 };
 
-// What a row's parts add up to, and the bins of its histogram: equal steps of
-// the score from the largest down to the smallest, or to where weights end.
+// What a row's parts add up to, and the bins of its histogram.
 struct RowStat {
-    float top, steps;
+    float top, low;
     uint32_t n;
-    __device__ __forceinline__ RowStat(const RowPart *part, int splits, float temperature) {
+    Bins bin;
+    __device__ __forceinline__ RowStat(const RowPart *part, int splits, float temperature)
+        : RowStat(total(part, splits), temperature) {}
+
+  private:
+    __device__ __forceinline__ RowStat(const RowPart &p, float temperature)
+        : top(p.top), low(p.low), n(p.n), bin(p.top, p.low, temperature, BINS) {}
+    static __device__ __forceinline__ RowPart total(const RowPart *part, int splits) {
         const int lane = threadIdx.x & 63;
-        const RowPart p = part[min(lane, splits - 1)];
-        float hi = p.top, lo = p.low;
+        RowPart p = part[min(lane, splits - 1)];
         int m = lane < splits ? (int)p.n : 0;
 #pragma unroll
         for (int s = 32; s >= 1; s >>= 1) {
-            hi = fmaxf(hi, __shfl_xor(hi, s, 64));
-            lo = fminf(lo, __shfl_xor(lo, s, 64));
+            p.top = fmaxf(p.top, __shfl_xor(p.top, s, 64));
+            p.low = fminf(p.low, __shfl_xor(p.low, s, 64));
             m += __shfl_xor(m, s, 64);
         }
-        top = hi;
-        n = (uint32_t)m;
-        steps = (float)(BINS - 2) / fmaxf(fminf(hi - lo, 44.0f * temperature), 1e-30f);
-    }
-    __device__ __forceinline__ int bin(float v) const {  // does not fall as the score falls
-        return v == top ? 0 : (int)fminf((top - v) * steps, (float)(BINS - 1));
+        p.n = (uint32_t)m;
+        return p;
     }
 };
 
@@ -557,7 +663,7 @@ __device__ __forceinline__ int boundary_bin(Shared<LONG_WAVES> &sh, const Sample
     for (int i = threadIdx.x; i < BINS; i += LONG_THREADS) sum += sh.hist[i] = w.hist[b * BINS + i];
     sum = block_sum<LONG_WAVES>(sh, sum);
     *want = COUNT ? (uint64_t)a.top_k : share(a.top_p, sum);
-    return (int)find_bin<LONG_WAVES>(sh, BINS, *want, over);
+    return (int)find_bin<BINS, LONG_WAVES>(sh, *want, over);
 }
 
 // The keys of the boundary's bin; with COUNT those of the bins before it too, so
@@ -642,11 +748,14 @@ __global__ __launch_bounds__(LONG_THREADS) void k_sample_sums(const E *__restric
         if (FORM == 1) {
             // (the list is the boundary's bin alone; the row stands for all bins)
             const uint64_t rest = listed ? want - over : want;
-            const uint32_t k = descend<WAVES>(sh, rest, [&](auto f) { each(f, weigh); }, &above);
+            const uint32_t k = n <= 64 ? few<WAVES>(sh, n, e.edge, rest, weigh, &above)
+                                       : descend<WAVES>(sh, rest, [&](auto f) { each(f, weigh); }, &above);
             e.by_weight(k, rest, above, weigh(k));
         } else {
             if ((uint64_t)a.top_k < st.n) {
-                const uint32_t k = descend<WAVES>(sh, (uint64_t)a.top_k, [&](auto f) { each(f, one); }, &above);
+                const uint32_t k =
+                    n <= 64 ? few<WAVES>(sh, n, e.edge, (uint64_t)a.top_k, one, &above)
+                            : descend<WAVES>(sh, (uint64_t)a.top_k, [&](auto f) { each(f, one); }, &above);
                 e.equal = (uint64_t)a.top_k - above;
                 e.edge = k;
             }
@@ -659,7 +768,8 @@ __global__ __launch_bounds__(LONG_THREADS) void k_sample_sums(const E *__restric
                 if (e.equal != ~0ull) sum += e.equal * weigh(e.edge);
                 want = share(a.top_p, sum);
                 // (the edge takes part with all its equals: one that step 1 cut has its own limit)
-                const uint32_t k = descend<WAVES>(sh, want, [&](auto f) { each(f, weigh); }, &above);
+                const uint32_t k = n <= 64 ? few<WAVES>(sh, n, e.edge, want, weigh, &above)
+                                           : descend<WAVES>(sh, want, [&](auto f) { each(f, weigh); }, &above);
                 e.by_weight(k, want, above, weigh(k));
             }
         }
@@ -691,7 +801,6 @@ __global__ __launch_bounds__(LONG_THREADS) void k_sample_pick(const E *__restric
                                                               int32_t *__restrict__ n_win) {
     constexpr int WAVES = LONG_WAVES;
     __shared__ Shared<WAVES> sh;
-    __shared__ RowSums sums[SPLITS * WAVES];
     const int64_t b = blockIdx.x;
     const int tid = threadIdx.x;
     const RowEdge re = w.edge[b];
@@ -703,7 +812,6 @@ __global__ __launch_bounds__(LONG_THREADS) void k_sample_pick(const E *__restric
     const RowStat st(w.part + b * w.splits, w.splits, a.temperature);
     const Weigher weigh = weigher<WAVES>(sh, a, key_of(st.top));
     const int ns = w.splits * WAVES;
-    if (tid < ns) sums[tid] = w.sums[b * ns + tid];
     __syncthreads();
     Edge e;
     e.edge = re.edge;
@@ -712,21 +820,9 @@ __global__ __launch_bounds__(LONG_THREADS) void k_sample_pick(const E *__restric
     uint64_t we = e.edge > 1 ? weigh(e.edge) : 0;
     we = we >= min_w ? we : 0;
     // kept weight and equal keys before each segment (a thread a segment)
-    const RowSums own = tid < ns ? sums[tid] : RowSums{0, 0};
-    const int lane = tid & 63, wv = tid >> 6;
-    const uint64_t si = wave_scan_u64(own.kept, lane), ei = wave_scan_u64(own.equal, lane);
-    if (lane == 63) {
-        sh.part[wv] = si;
-        sh.part2[wv] = ei;
-    }
-    __syncthreads();
-    uint64_t run = si - own.kept, eq = ei - own.equal, all = 0, eq_all = 0;
-    for (int q = 0; q < WAVES; ++q) {
-        run += q < wv ? sh.part[q] : 0;
-        eq += q < wv ? sh.part2[q] : 0;
-        all += sh.part[q];
-        eq_all += sh.part2[q];
-    }
+    const RowSums own = tid < ns ? w.sums[b * ns + tid] : RowSums{0, 0};
+    uint64_t run, eq, all, eq_all;
+    before_and_all<WAVES>(sh, own.kept, own.equal, &run, &eq, &all, &eq_all);
     const uint64_t target = target_of(u[b], all + (eq_all < e.equal ? eq_all : e.equal) * we);
     const uint64_t used = eq < e.equal ? eq : e.equal, left = e.equal - used;
     const uint64_t before = run + used * we, mine = own.kept + (own.equal < left ? own.equal : left) * we;
@@ -744,10 +840,10 @@ __global__ __launch_bounds__(LONG_THREADS) void k_sample_pick(const E *__restric
     const int64_t per = (g1 - g0 + LONG_THREADS - 1) / LONG_THREADS;
     const int64_t i0 = min(g1, g0 + tid * per), i1 = min(g1, i0 + per);
     int64_t at;
-    if (pick<WAVES>(sh, we, e, min_w, target, run, eq, i1 - i0, [&](int64_t i) {
+    if (pick<WAVES>(sh, weigh, we, e, min_w, target, run, eq, i1 - i0, [&](int64_t i) {
             const uint32_t k = key_of(as_float<E>(row.x[i0 + i]));
             return row.tf && row.tf[i0 + i] >= a.T ? 0u : k;
-        }, [&](int64_t, uint32_t k) { return weigh(k); }, &at))
+        }, &at))
         put_winner(winners, n_win, b, i0 + at, row.tf ? (int)row.tf[i0 + at] : 0, a);
 }
 
