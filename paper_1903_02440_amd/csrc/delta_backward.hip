@@ -234,12 +234,12 @@ struct GradLds {
     static constexpr int ONE = B::MT * (B::NT + 6) * FRAG;  // dO, Y, U of 32 columns
     static constexpr int TRI = B::TRI * 3 * FRAG;           // N, M, N^T, (beta M)^T: four of these
     static constexpr int SUMS = (2 * GRAD_WAVES + 2) * B::C * 4 + GRAD_WAVES * 4;
-    // K and Q take the room of the staged columns and of M and N as floats, once the
-    // four triangles are made, where they do not fit beside them
-    static constexpr int KQ = 2 * B::K, TEMP = ONE + 2 * SQ;
-    static constexpr bool APART = KQ + TEMP + 4 * TRI + SUMS + 8 * 1024 <= LDS_BYTES;
-    static constexpr int AT_KQ = APART ? TEMP : 0, R0 = APART ? TEMP + KQ : (KQ > TEMP ? KQ : TEMP);
-    static constexpr int AT_SQ = ONE, AT_TRI = R0, AT_SUMS = AT_TRI + 4 * TRI;
+    // M and N as floats take the room of the staged columns
+    static constexpr int TEMP = ONE > 2 * SQ ? ONE : 2 * SQ;
+    // K and Q, all of their groups of 32 of dk where they fit, else those of one pass of the waves
+    static constexpr bool WHOLE = TEMP + 2 * B::K + 4 * TRI + SUMS + 8192 <= LDS_BYTES;
+    static constexpr int GROUPS = WHOLE ? DS : GRAD_WAVES / 2, K = B::MT * GROUPS * B::NT * FRAG, KQ = 2 * K;
+    static constexpr int AT_KQ = TEMP, AT_TRI = AT_KQ + KQ, AT_SUMS = AT_TRI + 4 * TRI;
     static constexpr int AT_GAM = AT_SUMS + (SUMS + 15) / 16 * 16, BYTES = AT_GAM + B::C * 8 + 4 * B::C * 4;
 };
 
@@ -250,14 +250,14 @@ struct GradLds {
 // key head follow each other, so that their dq and dk add up in registers.
 template <class E, int DS>
 __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
-    const E *__restrict__ q, const E *__restrict__ k, const E *__restrict__ v, const float *__restrict__ g,
-    const E *__restrict__ d_out, Args a, const int32_t *__restrict__ lengths, Chunks w, Kept kept, E *__restrict__ d_q,
+    const E *__restrict__ v, const float *__restrict__ g, const E *__restrict__ d_out, Args a, const int32_t *__restrict__ lengths, Chunks w, Kept kept, E *__restrict__ d_q,
     E *__restrict__ d_k, E *__restrict__ d_v, float *__restrict__ d_g, float *__restrict__ d_beta) {
     using F = Blob<E, DS, true>;
     using G = GradLds<E, DS>;
     constexpr int C = F::C, MT = F::MT, NT = F::NT, GP = F::GP, PITCH = G::PITCH;
     constexpr int TW = (2 * DS + GRAD_WAVES - 1) / GRAD_WAVES;  // dk tiles of a wave
     constexpr int LT = MT * (MT + 1) / 2, LW = (2 * LT + GRAD_WAVES - 1) / GRAD_WAVES;  // tiles of M and N
+    constexpr int TASKS = (3 * MT + GRAD_WAVES - 1) / GRAD_WAVES;                        // tiles of Y, U and dO
     extern __shared__ char lds[];
     const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, gr = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
     const int n = (lengths ? max(0, min(a.L, lengths[b])) : a.L) - chunk * C;
     if (n <= 0) return;
     char *fo = lds, *fy = fo + MT * NT * FRAG, *fu = fy + MT * 3 * FRAG;
-    float *sqM = reinterpret_cast<float *>(lds + G::AT_SQ), *sqN = sqM + C * PITCH;
+    float *sqM = reinterpret_cast<float *>(lds), *sqN = sqM + C * PITCH;
     char *tri = lds + G::AT_TRI;  // N, M, N^T, (beta M)^T
     float *sums = reinterpret_cast<float *>(lds + G::AT_SUMS);  // [waves][2][C], then y.v, beta; then the ends
     float *yv = sums + 2 * GRAD_WAVES * C, *ends = yv + 2 * C;
@@ -274,8 +274,19 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
     const char *key = w.key + ((int64_t)blockIdx.y * w.NC + chunk) * F::KEY;
     const int64_t row0 = (int64_t)b * a.L + chunk * C;
 
-    const char *fk = lds + G::AT_KQ, *fq = fk + F::K;
-    if (G::APART) to_lds(lds + G::AT_KQ, key, G::KQ, wv, GRAD_WAVES, lane);
+    const char *fk = lds + G::AT_KQ, *fq = fk + G::K;
+    // groups of dk from s0 on of K and Q
+    auto fetch = [&](int s0) {
+        if (G::WHOLE) {
+            to_lds(lds + G::AT_KQ, key, G::KQ, wv, GRAD_WAVES, lane);
+        } else {
+#pragma unroll
+            for (int x = 0; x < 2 * MT; ++x)  // K's tiles of samples, then Q's
+                to_lds(lds + G::AT_KQ + x * G::GROUPS * NT * FRAG, key + (x * DS + s0) * NT * FRAG, G::GROUPS * NT * FRAG, wv,
+                       GRAD_WAVES, lane);
+        }
+    };
+    if (G::WHOLE) fetch(0);
 
     f32x4 dqs[TW][MT], dks[TW][MT];
 #pragma unroll
@@ -308,54 +319,82 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
         for (int l = 0; l < LW; ++l) mn[l] = (f32x4){0.f, 0.f, 0.f, 0.f};
         float dot = 0.0f;   // <dS, S>, the lane's part
         float yvp = 0.0f;   // y.v of row 16 wv + m, the lane's part (waves below MT)
+        // The wave's share of the next 32 columns is on its way while these are used:
+        // Y, U and dO by tile of samples (Y of tile mt: wave mt), v beside Y, and the
+        // rows of S and dS that are its right operands.
+        f32x4 sn[TW][2], en[TW][2], yu[TASKS][2];
+        E vo[TASKS][8];
+        auto load = [&](int vg) {
+#pragma unroll
+            for (int p = 0; p < TW; ++p) {
+                const int t = min(p * GRAD_WAVES + wv, 2 * DS - 1);
+                const float *ps = S + (int64_t)dk_of(t, m) * kept.dvp + 32 * vg + 4 * gr;
+                const float *pd = dS + (int64_t)dk_of(t, m) * kept.dvp + 32 * vg + 4 * gr;
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) {
+                    sn[p][hf] = *reinterpret_cast<const f32x4 *>(ps + 16 * hf);
+                    en[p][hf] = *reinterpret_cast<const f32x4 *>(pd + 16 * hf);
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < TASKS; ++x) {
+                const int task = min(wv + x * GRAD_WAVES, 3 * MT - 1), which = task / MT, i = 16 * (task % MT) + m;
+                const float *pf = (which == 1 ? U : Y) + (int64_t)i * kept.dvp + 32 * vg + 4 * gr;
+                const E *pe = (which == 2 ? d_out : v) + ((row0 + min(i, n - 1)) * a.Hv + h) * a.dv;
+                if (which < 2) {
+                    yu[x][0] = *reinterpret_cast<const f32x4 *>(pf);
+                    yu[x][1] = *reinterpret_cast<const f32x4 *>(pf + 16);
+                }
+                if (which != 1) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) vo[x][j] = pe[min(32 * vg + slot(gr, j), a.dv - 1)];
+                }
+            }
+        };
+        load(0);
         for (int vg = 0; vg < kept.dvp / 32; ++vg) {
             __syncthreads();  // the staged columns (and, at first, the coefficients) may be written
-            for (int task = wv; task < 3 * MT; task += GRAD_WAVES) {
-                const int which = task / MT, mt = task % MT, i = 16 * mt + m;  // Y, U, dO (Y of tile mt: wave mt)
-                float x[8];
-                if (which < 2) {
-                    const float *p = (which ? U : Y) + (int64_t)i * kept.dvp + 32 * vg + 4 * gr;
-                    const f32x4 x0 = *reinterpret_cast<const f32x4 *>(p), x1 = *reinterpret_cast<const f32x4 *>(p + 16);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) x[r] = x0[r], x[4 + r] = x1[r];
-                    put_frag<3>((which ? fu : fy) + mt * 3 * FRAG, lane, split<3>(x));
+            for (int x = 0; x < TASKS; ++x) {
+                const int task = wv + x * GRAD_WAVES, which = task / MT, mt = task % MT, i = 16 * mt + m;
+                if (task >= 3 * MT) continue;
+                float y[8];
+                if (which < 2) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) y[j] = yu[x][j >> 2][j & 3];
+                    put_frag<3>((which ? fu : fy) + mt * 3 * FRAG, lane, split<3>(y));
                     if (which == 0) {
                         const int64_t vrow = ((row0 + min(i, n - 1)) * a.Hv + h) * a.dv;
                         const float be = co[C + i];
-                        E ve[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) ve[j] = v[vrow + min(32 * vg + slot(gr, j), a.dv - 1)];
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
                             const int cv = 32 * vg + slot(gr, j);
                             const bool in = i < n && cv < a.dv;
-                            yvp += in ? x[j] * to_float(ve[j]) : 0.0f;
-                            if (in) d_v[vrow + cv] = from_float<E>(be * x[j]);
+                            yvp += in ? y[j] * to_float(vo[x][j]) : 0.0f;
+                            if (in) d_v[vrow + cv] = from_float<E>(be * y[j]);
                         }
                     }
                 } else {
-                    const int64_t vrow = ((row0 + min(i, n - 1)) * a.Hv + h) * a.dv;
-                    E oe[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) oe[j] = d_out[vrow + min(32 * vg + slot(gr, j), a.dv - 1)];
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        x[j] = i < n && 32 * vg + slot(gr, j) < a.dv ? to_float(oe[j]) : 0.0f;
-                    put_frag<NT>(fo + mt * NT * FRAG, lane, split<NT>(x));
+                        y[j] = i < n && 32 * vg + slot(gr, j) < a.dv ? to_float(vo[x][j]) : 0.0f;
+                    put_frag<NT>(fo + mt * NT * FRAG, lane, split<NT>(y));
                 }
             }
+            f32x4 sc[TW][2], ec[TW][2];
+#pragma unroll
+            for (int p = 0; p < TW; ++p)
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) sc[p][hf] = sn[p][hf], ec[p][hf] = en[p][hf];
             __syncthreads();
+            if (vg + 1 < kept.dvp / 32) load(vg + 1);
 #pragma unroll
             for (int p = 0; p < TW; ++p) {
                 const int t = p * GRAD_WAVES + wv;
                 if (t >= 2 * DS) continue;
-                const float *ps = S + (int64_t)dk_of(t, m) * kept.dvp + 32 * vg + 4 * gr;
-                const float *pd = dS + (int64_t)dk_of(t, m) * kept.dvp + 32 * vg + 4 * gr;
-                const f32x4 s0 = *reinterpret_cast<const f32x4 *>(ps), s1 = *reinterpret_cast<const f32x4 *>(ps + 16);
-                const f32x4 e0 = *reinterpret_cast<const f32x4 *>(pd), e1 = *reinterpret_cast<const f32x4 *>(pd + 16);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) dot += s0[r] * e0[r] + s1[r] * e1[r];
-                const Terms<3> st = split<3>(s0, s1), et = split<3>(e0, e1);
+                for (int r = 0; r < 4; ++r) dot += sc[p][0][r] * ec[p][0][r] + sc[p][1][r] * ec[p][1][r];
+                const Terms<3> st = split<3>(sc[p][0], sc[p][1]), et = split<3>(ec[p][0], ec[p][1]);
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {
                     mma<NT, 3>(dq[p][mt], frag<NT>(fo + mt * NT * FRAG, lane), st);
@@ -373,6 +412,7 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
                 else mma<NT, 3>(mn[l], frag<NT>(fo + mt * NT * FRAG, lane), frag<3>(fu + nt * 3 * FRAG, lane));
             }
         }
+        __syncthreads();  // the staged columns are done with
 #pragma unroll
         for (int l = 0; l < LW; ++l) {
             const int idx = l * GRAD_WAVES + wv;
@@ -412,8 +452,7 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
             put_frag<3>(tri + which * G::TRI + f * 3 * FRAG, lane, split<3>(x));
         }
         __syncthreads();
-        if (!G::APART) to_lds(lds + G::AT_KQ, key, G::KQ, wv, GRAD_WAVES, lane);
-        if (!G::APART || hr == 0) {
+        if (G::WHOLE && hr == 0) {  // K and Q have come
             wait_copies();
             lds_barrier();
         }
@@ -424,22 +463,19 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
             for (int r = 0; r < 4; ++r) pg[mt][r] = pb[mt][r] = 0.0f;
 #pragma unroll
         for (int p = 0; p < TW; ++p) {
-            const int t = p * GRAD_WAVES + wv, d = dk_of(t, m);
+            const int t = p * GRAD_WAVES + wv, tl = G::WHOLE ? t : wv;  // (tl: in what LDS has of K and Q)
+            if (!G::WHOLE) {
+                lds_barrier();
+                fetch(p * G::GROUPS);
+                wait_copies();
+                lds_barrier();
+            }
             if (t >= 2 * DS) continue;
-            E ke[MT][4], qe[MT][4];
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int64_t at = ((row0 + min(16 * mt + 4 * gr + r, n - 1)) * a.Hk + hk) * a.dk + min(d, a.dk - 1);
-                    ke[mt][r] = k[at];
-                    qe[mt][r] = q[at];
-                }
             Terms<NT> kt[GP], qt[GP];
 #pragma unroll
             for (int gp = 0; gp < GP; ++gp) {
-                kt[gp] = tfrag<NT, DS>(fk, t, gp, lane);
-                qt[gp] = tfrag<NT, DS>(fq, t, gp, lane);
+                kt[gp] = tfrag<NT, G::GROUPS>(fk, tl, gp, lane);
+                qt[gp] = tfrag<NT, G::GROUPS>(fq, tl, gp, lane);
             }
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
@@ -447,12 +483,17 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
                 const f32x4 be = *reinterpret_cast<const f32x4 *>(co + C + 16 * mt + 4 * gr);
                 const f32x4 la = *reinterpret_cast<const f32x4 *>(co + 2 * C + 16 * mt + 4 * gr);
                 f32x4 x = a.scale * ev * dq[p][mt], y = (f32x4){0.f, 0.f, 0.f, 0.f} - ev * rr[p][mt], z = la * cc[p][mt];
-                float kk[4], qq[4];
+                float kk[4], qq[4];  // k and q at the tile's places
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const bool in = 16 * mt + 4 * gr + r < n && d < a.dk;
-                    kk[r] = in ? to_float(ke[mt][r]) : 0.0f;
-                    qq[r] = in ? to_float(qe[mt][r]) : 0.0f;
+                    kk[r] = qq[r] = 0.0f;
+#pragma unroll
+                    for (int x = 0; x < NT; ++x) {
+                        const int o = ((mt * G::GROUPS + (tl >> 1)) * NT + x) * FRAG +
+                                      ((m >> 2) * 16 + 4 * gr + r) * 16 + (4 * (tl & 1) + (m & 3)) * 2;
+                        kk[r] += to_float(*reinterpret_cast<const uint16_t *>(fk + o));
+                        qq[r] += to_float(*reinterpret_cast<const uint16_t *>(fq + o));
+                    }
                     pe += kk[r] * z[r];
                 }
                 f32x4 mk = {0.f, 0.f, 0.f, 0.f}, mc = mk;
@@ -589,7 +630,7 @@ int backward(const Call &c, const Args &a, void *ws, hipStream_t st, const char 
     launch_rscan<E, DS, KS>(cols, d_out, a, c.lengths, w, kept, c.d_last, c.d_first, st)
     SPK_DELTA_PARTS(DS, cols, SPK_SCAN)
 #undef SPK_SCAN
-    hipLaunchKernelGGL((k_delta_grads<E, DS>), per_key, dim3(GRAD_THREADS), LG, st, q, k, v, c.g, d_out, a, c.lengths, w, kept, static_cast<E *>(c.d_q), static_cast<E *>(c.d_k),
+    hipLaunchKernelGGL((k_delta_grads<E, DS>), per_key, dim3(GRAD_THREADS), LG, st, v, c.g, d_out, a, c.lengths, w, kept, static_cast<E *>(c.d_q), static_cast<E *>(c.d_k),
                        static_cast<E *>(c.d_v), c.d_g, c.d_beta);
     return spk::check_launch(name);
 }
