@@ -225,6 +225,11 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
         }
 }
 
+template <class E>
+struct alignas(4 * sizeof(E)) Four {
+    E e[4];
+};
+
 constexpr int GRAD_WAVES = 8, GRAD_THREADS = GRAD_WAVES * 64;
 
 template <class E, int DS>
@@ -250,7 +255,8 @@ struct GradLds {
 // key head follow each other, so that their dq and dk add up in registers.
 template <class E, int DS>
 __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
-    const E *__restrict__ v, const float *__restrict__ g, const E *__restrict__ d_out, Args a, const int32_t *__restrict__ lengths, Chunks w, Kept kept, E *__restrict__ d_q,
+    const E *__restrict__ v, const float *__restrict__ g, const E *__restrict__ d_out, Args a,
+    const int32_t *__restrict__ lengths, int wide, Chunks w, Kept kept, E *__restrict__ d_q,
     E *__restrict__ d_k, E *__restrict__ d_v, float *__restrict__ d_g, float *__restrict__ d_beta) {
     using F = Blob<E, DS, true>;
     using G = GradLds<E, DS>;
@@ -323,8 +329,8 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
         // Y, U and dO by tile of samples (Y of tile mt: wave mt), v beside Y, and the
         // rows of S and dS that are its right operands.
         f32x4 sn[TW][2], en[TW][2], yu[TASKS][2];
-        E vo[TASKS][8];
-        auto load = [&](int vg) {
+        Four<E> vo[TASKS][2];
+        auto load_states = [&](int vg) {
 #pragma unroll
             for (int p = 0; p < TW; ++p) {
                 const int t = min(p * GRAD_WAVES + wv, 2 * DS - 1);
@@ -336,6 +342,9 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
                     en[p][hf] = *reinterpret_cast<const f32x4 *>(pd + 16 * hf);
                 }
             }
+        };
+        auto load = [&](int vg) {
+            if (TW == 1) load_states(vg);  // (two tiles a wave have no registers to spare for it)
 #pragma unroll
             for (int x = 0; x < TASKS; ++x) {
                 const int task = min(wv + x * GRAD_WAVES, 3 * MT - 1), which = task / MT, i = 16 * (task % MT) + m;
@@ -346,8 +355,14 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
                     yu[x][1] = *reinterpret_cast<const f32x4 *>(pf + 16);
                 }
                 if (which != 1) {
+                    if (wide) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) vo[x][j] = pe[min(32 * vg + slot(gr, j), a.dv - 1)];
+                        for (int hf = 0; hf < 2; ++hf)
+                            vo[x][hf] = *reinterpret_cast<const Four<E> *>(pe + min(32 * vg + 16 * hf + 4 * gr, a.dv - 4));
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) vo[x][j >> 2].e[j & 3] = pe[min(32 * vg + slot(gr, j), a.dv - 1)];
+                    }
                 }
             }
         };
@@ -366,21 +381,33 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
                     if (which == 0) {
                         const int64_t vrow = ((row0 + min(i, n - 1)) * a.Hv + h) * a.dv;
                         const float be = co[C + i];
+                        Four<E> dv4[2];
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
-                            const int cv = 32 * vg + slot(gr, j);
-                            const bool in = i < n && cv < a.dv;
-                            yvp += in ? y[j] * to_float(vo[x][j]) : 0.0f;
-                            if (in) d_v[vrow + cv] = from_float<E>(be * y[j]);
+                            const bool in = i < n && 32 * vg + slot(gr, j) < a.dv;
+                            yvp += in ? y[j] * to_float(vo[x][j >> 2].e[j & 3]) : 0.0f;
+                            dv4[j >> 2].e[j & 3] = from_float<E>(be * y[j]);
+                        }
+#pragma unroll
+                        for (int hf = 0; hf < 2; ++hf) {
+                            const int cv = 32 * vg + 16 * hf + 4 * gr;
+                            if (wide) {
+                                if (i < n && cv < a.dv) *reinterpret_cast<Four<E> *>(d_v + vrow + cv) = dv4[hf];
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 4; ++j)
+                                    if (i < n && cv + j < a.dv) d_v[vrow + cv + j] = dv4[hf].e[j];
+                            }
                         }
                     }
                 } else {
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        y[j] = i < n && 32 * vg + slot(gr, j) < a.dv ? to_float(vo[x][j]) : 0.0f;
+                        y[j] = i < n && 32 * vg + slot(gr, j) < a.dv ? to_float(vo[x][j >> 2].e[j & 3]) : 0.0f;
                     put_frag<NT>(fo + mt * NT * FRAG, lane, split<NT>(y));
                 }
             }
+            if (TW > 1) load_states(vg);
             f32x4 sc[TW][2], ec[TW][2];
 #pragma unroll
             for (int p = 0; p < TW; ++p)
@@ -630,7 +657,10 @@ int backward(const Call &c, const Args &a, void *ws, hipStream_t st, const char 
     launch_rscan<E, DS, KS>(cols, d_out, a, c.lengths, w, kept, c.d_last, c.d_first, st)
     SPK_DELTA_PARTS(DS, cols, SPK_SCAN)
 #undef SPK_SCAN
-    hipLaunchKernelGGL((k_delta_grads<E, DS>), per_key, dim3(GRAD_THREADS), LG, st, v, c.g, d_out, a, c.lengths, w, kept, static_cast<E *>(c.d_q), static_cast<E *>(c.d_k),
+    const bool fours = ((reinterpret_cast<uintptr_t>(c.v) | reinterpret_cast<uintptr_t>(c.d_out) |
+                         reinterpret_cast<uintptr_t>(c.d_v)) & (4 * sizeof(E) - 1)) == 0;
+    const int wide = a.dv % 4 == 0 && fours;  // rows of dv elements go four at a time
+    hipLaunchKernelGGL((k_delta_grads<E, DS>), per_key, dim3(GRAD_THREADS), LG, st, v, c.g, d_out, a, c.lengths, wide, w, kept, static_cast<E *>(c.d_q), static_cast<E *>(c.d_k),
                        static_cast<E *>(c.d_v), c.d_g, c.d_beta);
     return spk::check_launch(name);
 }
