@@ -11,7 +11,7 @@ from __future__ import annotations
 
 import torch
 
-from . import _F, _I, _P, _Z, _check, _lib, _need, _out, _ptr, _stream, _ws
+from . import _F, _I, _P, _Z, _check, _lib, _need, _out, _ws
 
 _SIGS = {
     "spk_delta_rule_workspace_size": (_Z, [_I] * 7),
@@ -34,21 +34,30 @@ __all__ = ["SPK_F32", "SPK_BF16"] + list(_SIGS)
 
 
 def _dtype(t, name):
-    if t.dtype not in _DTYPES:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
         raise TypeError(f"{name}: expected torch.float32 or torch.bfloat16, got {t.dtype}")
-    return _DTYPES[t.dtype]
+    return code
 
 
-def _same_device(dev, **tensors):
-    for name, t in tensors.items():
-        if isinstance(t, torch.Tensor) and t.device != dev:
-            raise ValueError(f"{name}: on {t.device}, the call's tensors are on {dev}")
+def _at(dev, name, t):
+    """Address of a tensor on the call's device (None and False: NULL)."""
+    if t is None or t is False:
+        return None
+    if t.device != dev:
+        raise ValueError(f"{name}: on {t.device}, the call's tensors are on {dev}")
+    if not t.is_contiguous():
+        raise ValueError("libspyke needs contiguous tensors")
+    return t.data_ptr()
 
 
 def _on(dev, stream, call):
-    """call(stream pointer) with `dev` current (a launch goes to the current device)."""
+    """call(stream handle) with `dev` current (a launch goes to the current device)."""
+    if dev.index == torch.cuda.current_device():
+        _check(call(stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(dev.index)))
+        return
     with torch.cuda.device(dev):
-        _check(call(_stream(stream)))
+        _check(call(stream.cuda_stream if stream is not None else torch.cuda.current_stream(dev).cuda_stream))
 
 
 # ---------------------------------------------------------------- delta rule
@@ -99,11 +108,10 @@ def spk_delta_rule(q, k, v, g, beta, scale=1.0, initial_state=None, lengths=None
     final_state = _out(final_state, (B, Hv, dk, dv), torch.float32, dev, "final_state")
     n = spk_delta_rule_workspace_size(dt, B, L, Hk, Hv, dk, dv)
     ws = _ws(workspace, n, dev)
-    _same_device(dev, k=k, v=v, g=g, beta=beta, lengths=lengths, initial_state=initial_state, out=out,
-                 final_state=final_state, workspace=ws)
-    _on(dev, stream, lambda st: _lib.spk_delta_rule(
-        _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), dt, B, L, Hk, Hv, dk, dv, float(scale), _ptr(lengths),
-        _ptr(initial_state), _ptr(out), _ptr(final_state), _ptr(ws), n, st))
+    args = (_at(dev, "q", q), _at(dev, "k", k), _at(dev, "v", v), _at(dev, "g", g), _at(dev, "beta", beta), dt, B, L,
+            Hk, Hv, dk, dv, scale, _at(dev, "lengths", lengths), _at(dev, "initial_state", initial_state),
+            _at(dev, "out", out), _at(dev, "final_state", final_state), _at(dev, "workspace", ws), n)
+    _on(dev, stream, lambda st: _lib.spk_delta_rule(*args, st))
     return out, (final_state if final_state is not False else None)
 
 
@@ -122,11 +130,11 @@ def spk_delta_rule_step(q, k, v, g, beta, state, scale=1.0, out=None, stream=Non
     _need(g, torch.float32, (B, Hv), "g")
     _need(beta, torch.float32, (B, Hv), "beta")
     _need(state, torch.float32, (B, Hv, dk, dv), "state")
-    out = _out(out, (B, Hv, dv), q.dtype, q.device, "out")
-    _same_device(q.device, k=k, v=v, g=g, beta=beta, state=state, out=out)
-    _on(q.device, stream, lambda st: _lib.spk_delta_rule_step(
-        _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), dt, B, Hk, Hv, dk, dv, float(scale), _ptr(state), _ptr(out),
-        st))
+    dev = q.device
+    out = _out(out, (B, Hv, dv), q.dtype, dev, "out")
+    args = (_at(dev, "q", q), _at(dev, "k", k), _at(dev, "v", v), _at(dev, "g", g), _at(dev, "beta", beta), dt, B, Hk,
+            Hv, dk, dv, scale, _at(dev, "state", state), _at(dev, "out", out))
+    _on(dev, stream, lambda st: _lib.spk_delta_rule_step(*args, st))
     return out
 
 
@@ -149,13 +157,12 @@ def spk_delta_rule_backward(q, k, v, g, beta, d_out, d_final_state=None, scale=1
     d_initial_state = _out(d_initial_state, state, f32, dev, "d_initial_state")
     n = spk_delta_rule_backward_workspace_size(dt, B, L, Hk, Hv, dk, dv)
     ws = _ws(workspace, n, dev)
-    _same_device(dev, k=k, v=v, g=g, beta=beta, lengths=lengths, initial_state=initial_state, d_out=d_out,
-                 d_final_state=d_final_state, d_q=d_q, d_k=d_k, d_v=d_v, d_g=d_g, d_beta=d_beta,
-                 d_initial_state=d_initial_state, workspace=ws)
-    _on(dev, stream, lambda st: _lib.spk_delta_rule_backward(
-        _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), dt, B, L, Hk, Hv, dk, dv, float(scale), _ptr(lengths),
-        _ptr(initial_state), _ptr(d_out), _ptr(d_final_state), _ptr(d_q), _ptr(d_k), _ptr(d_v), _ptr(d_g),
-        _ptr(d_beta), _ptr(d_initial_state), _ptr(ws), n, st))
+    args = (_at(dev, "q", q), _at(dev, "k", k), _at(dev, "v", v), _at(dev, "g", g), _at(dev, "beta", beta), dt, B, L,
+            Hk, Hv, dk, dv, scale, _at(dev, "lengths", lengths), _at(dev, "initial_state", initial_state),
+            _at(dev, "d_out", d_out), _at(dev, "d_final_state", d_final_state), _at(dev, "d_q", d_q),
+            _at(dev, "d_k", d_k), _at(dev, "d_v", d_v), _at(dev, "d_g", d_g), _at(dev, "d_beta", d_beta),
+            _at(dev, "d_initial_state", d_initial_state), _at(dev, "workspace", ws), n)
+    _on(dev, stream, lambda st: _lib.spk_delta_rule_backward(*args, st))
     return d_q, d_k, d_v, d_g, d_beta, (d_initial_state if d_initial_state is not False else None)
 
 
@@ -182,8 +189,8 @@ def spk_sample_winners(scores, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0
     n_winners = _out(n_winners, (B,), torch.int32, dev, "n_winners")
     n = spk_sample_winners_workspace_size(dt, B, C, H, W)
     ws = _ws(workspace, n, dev)
-    _same_device(dev, u=u, t_first=t_first, winners=winners, n_winners=n_winners, workspace=ws)
-    _on(dev, stream, lambda st: _lib.spk_sample_winners(
-        _ptr(scores), dt, _ptr(t_first), _ptr(u), B, int(T), C, H, W, float(temperature), int(top_k), float(top_p),
-        float(min_p), _ptr(winners), _ptr(n_winners), _ptr(ws), n, st))
+    args = (_at(dev, "scores", scores), dt, _at(dev, "t_first", t_first), _at(dev, "u", u), B, T, C, H, W, temperature,
+            top_k, top_p, min_p, _at(dev, "winners", winners), _at(dev, "n_winners", n_winners),
+            _at(dev, "workspace", ws), n)
+    _on(dev, stream, lambda st: _lib.spk_sample_winners(*args, st))
     return winners, n_winners
