@@ -190,6 +190,7 @@ extern "C" int spk_delta_rule(const void *q, const void *k, const void *v, const
         const size_t need = chunk_workspace(a);
         SPK_REQUIRE(workspace && ws_bytes >= need, SPK_E_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", name,
                     workspace ? ws_bytes : (size_t)0, need);
+        SPK_REQUIRE(aligned16(workspace), SPK_E_ARG, "%s: the workspace must be 16-byte aligned", name);
         return chunk_forward(q, k, v, g, beta, a, lengths, initial_state, out, final_state, workspace, st, name);
     }
     if (dtype == SPK_F32) launch_seq<float>(q, k, v, g, beta, a, lengths, initial_state, out, final_state, st);

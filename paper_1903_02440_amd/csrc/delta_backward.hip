@@ -721,6 +721,7 @@ extern "C" int spk_delta_rule_backward(const void *q, const void *k, const void 
     const size_t need = workspace_bytes(a);
     SPK_REQUIRE(workspace && ws_bytes >= need, SPK_E_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", name,
                 workspace ? ws_bytes : (size_t)0, need);
+    SPK_REQUIRE(aligned16(workspace), SPK_E_ARG, "%s: the workspace must be 16-byte aligned", name);
     const Call c{q, k, v, g, beta, lengths, initial_state, d_out, d_final_state, d_q, d_k, d_v, d_g, d_beta,
                  d_initial_state};
     return run(c, a, workspace, st, name);

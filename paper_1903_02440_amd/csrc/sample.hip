@@ -941,6 +941,8 @@ extern "C" int spk_sample_winners(const void *scores, int dtype, const uint8_t *
     const size_t need = spk_sample_winners_workspace_size(dtype, B, C, H, W);
     SPK_REQUIRE(need == 0 || (workspace && ws_bytes >= need), SPK_E_WORKSPACE, "%s: workspace of %zu bytes, %zu needed",
                 name, workspace ? ws_bytes : (size_t)0, need);
+    SPK_REQUIRE(need == 0 || (reinterpret_cast<uintptr_t>(workspace) & 15) == 0, SPK_E_ARG,
+                "%s: the workspace must be 16-byte aligned", name);
     SampleArgs a;
     a.N = (int64_t)C * H * W;
     a.T = T;

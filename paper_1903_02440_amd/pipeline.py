@@ -29,6 +29,13 @@ calls on one stream, with no host synchronisation and no allocation inside
   (``spk_stdp_first_spike`` / ``spk_rstdp_first_spike``); only a conv stage
   fed by another conv still writes per-step spikes;
 * after a reward-modulated last layer: ``spk_decide``;
+* with ``sample=dict(temperature=..., top_k=..., top_p=..., min_p=...)`` the
+  last conv stage's one winner is drawn by its neurons' potentials
+  (``spk_sample_winners`` in the place of ``spk_kwta``), with a uniform number
+  per image from :meth:`Chain.set_input`: a reward-modulated layer then explores
+  other decisions than its best, and learns from what it drew.  Its neurons have
+  to fire at one step (the infinite threshold) for the draw to leave the spikes'
+  order out;
 * learning: ``spk_stdp`` / ``spk_rstdp`` per conv stage (frozen forward,
   ordered replay within the batch).  The layers' updates touch disjoint
   weights, so with ``concurrent_learn`` they run on side streams (default
@@ -54,7 +61,7 @@ from . import (pool_out_size, conv_out_size, spk_conv_fire, spk_conv_fire_first_
                spk_rstdp_strided, spk_stdp_strided, spk_stdp_first_spike, spk_rstdp_first_spike, spk_decide,
                spk_encode_latency, spk_encode_latency_workspace_size, spk_kwta, spk_kwta_workspace_size,
                spk_local_normalization, spk_pool, spk_pool_first_spike, spk_rank_latency, spk_rstdp, spk_stdp,
-               spk_stdp_workspace_size)
+               spk_stdp_workspace_size, spk_sample_winners, spk_sample_winners_workspace_size)
 
 
 def _is_conv(st):
@@ -68,7 +75,8 @@ def _stride(st):
 class Chain:
     def __init__(self, stages, B, T, H, W, cin, source="image", filter_bank=None, filter_threshold=0.0,
                  n_classes=10, device="cuda", want_potentials=True, pool_from_first_spike=True,
-                 concurrent_learn=True, want_spikes=True, local_norm=None, fused=False, want_waves=True):
+                 concurrent_learn=True, want_spikes=True, local_norm=None, fused=False, want_waves=True,
+                 sample=None):
         self.stages = [copy.copy(st) for st in stages]  # own copies: set_rates changes them
         self.fused = fused
         # without waves, the encoder's and the pools' outputs are first-spike maps only
@@ -132,6 +140,15 @@ class Chain:
                 h, w = ho, wo
             b["shape_in"] = None
             self.bufs.append(b)
+        # sample: settings of the draw that takes the place of the last conv stage's kWTA
+        self.sample = None if sample is None else dict(sample)
+        if sample is not None:
+            last = self.conv_stages()[-1]
+            st, tf = self.stages[last], self.bufs[last]["tf"]
+            if st.k != 1 or not math.isinf(st.thr):
+                raise ValueError("sample needs a last conv stage with k = 1 and the infinite threshold")
+            ws_bytes = max(ws_bytes, spk_sample_winners_workspace_size(0, B, *tf.shape[1:]))
+            self.uniform = torch.zeros((B,), dtype=f32, device=dev)
         self.workspace = torch.empty(max(ws_bytes, 256), dtype=u8, device=dev)
         self.labels = torch.zeros((B,), dtype=i32, device=dev)
         self.decision = torch.empty((B,), dtype=i32, device=dev)
@@ -182,19 +199,22 @@ class Chain:
         st = self.stages[self.conv_stages()[layer]]
         return st.a_plus, st.a_minus
 
-    def set_input(self, image=None, wave=None, labels=None):
+    def set_input(self, image=None, wave=None, labels=None, uniform=None):
         if image is not None:
             self.image.copy_(image)
         if wave is not None:
             self.input_wave.copy_(wave)
         if labels is not None:
             self.labels.copy_(labels)
+        if uniform is not None:
+            self.uniform.copy_(uniform)
 
     # ---------------------------------------------------------------- run
     def forward(self, stream=None, hook=None, early_learn=False):
         """Enqueue the forward of the batch.  hook(name, phase), if given, is
         called right before (phase 0) and after (phase 1) each C-ABI call;
-        names are "encode", "conv<i>", "kwta<i>", "pool<i>", "decide"."""
+        names are "encode", "conv<i>", "kwta<i>" ("draw<i>" with sample), "pool<i>",
+        "decide"."""
         mark = hook or (lambda name, phase: None)
         main = stream if stream is not None else torch.cuda.current_stream()
         self._wait_pending(-1, main)
@@ -252,6 +272,11 @@ class Chain:
                         spk_kwta(b["tf"], b["vf"], self.T, st.k, st.r, winners=b["win"], n_winners=b["nw"],
                                  workspace=b["ws_kwta"], stream=side)
                         mark(f"kwta{i}", 1)
+                elif self.sample is not None and i == self.conv_stages()[-1]:
+                    mark(f"draw{i}", 0)
+                    spk_sample_winners(b["vf"], self.uniform, t_first=b["tf"], T=self.T, winners=b["win"],
+                                       n_winners=b["nw"], workspace=self.workspace, stream=stream, **self.sample)
+                    mark(f"draw{i}", 1)
                 else:
                     mark(f"kwta{i}", 0)
                     spk_kwta(b["tf"], b["vf"], self.T, st.k, st.r, winners=b["win"], n_winners=b["nw"],
@@ -406,15 +431,16 @@ class OnlineTrainer:
     runs eagerly.  Weights change in place (chain.weights())."""
 
     def __init__(self, stages, T, H, W, cin, filter_bank, filter_threshold=0.0, n_classes=10, device="cuda",
-                 use_graph=True, steps_per_graph=16):
+                 use_graph=True, steps_per_graph=16, sample=None):
         self.chain = Chain(stages, 1, T, H, W, cin, source="image", filter_bank=filter_bank,
                            filter_threshold=filter_threshold, n_classes=n_classes, device=device,
-                           want_potentials=False, want_spikes=False, concurrent_learn=False)
+                           want_potentials=False, want_spikes=False, concurrent_learn=False, sample=sample)
         dev = self.chain.image.device
         self.use_graph = use_graph
         self.K = max(1, int(steps_per_graph))
         self.img_stage = torch.zeros((self.K, H, W), dtype=torch.uint8, device=dev)
         self.lab_stage = torch.zeros((self.K,), dtype=torch.int32, device=dev)
+        self.uni_stage = torch.zeros((self.K,), dtype=torch.float32, device=dev) if sample is not None else None
         self.graph = None
 
     def set_weights(self, weights):
@@ -432,6 +458,8 @@ class OnlineTrainer:
     def _step_from(self, j):
         self.chain.image.copy_(self.img_stage[j:j + 1])
         self.chain.labels.copy_(self.lab_stage[j:j + 1])
+        if self.uni_stage is not None:
+            self.chain.uniform.copy_(self.uni_stage[j:j + 1])
         self.chain.step()
 
     def _capture(self):
@@ -451,9 +479,10 @@ class OnlineTrainer:
                 self._step_from(j)
         self.graph = g
 
-    def run(self, images, labels=None):
+    def run(self, images, labels=None, uniform=None):
         """Learn from images (u8 [N, H, W] on the device) in order; labels
-        (i32 [N]) feed the decision of a reward-modulated last layer."""
+        (i32 [N]) feed the decision of a reward-modulated last layer, and
+        uniform (f32 [N] in [0, 1)) the draw of its winner with `sample`."""
         N = images.shape[0]
         i = 0
         while i < N:
@@ -461,6 +490,8 @@ class OnlineTrainer:
             self.img_stage[:n].copy_(images[i:i + n])
             if labels is not None:
                 self.lab_stage[:n].copy_(labels[i:i + n])
+            if uniform is not None:
+                self.uni_stage[:n].copy_(uniform[i:i + n])
             if self.use_graph and n == self.K:
                 if self.graph is None:
                     self._capture()

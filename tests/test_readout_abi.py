@@ -149,3 +149,20 @@ def test_workspace_sizes():
     # the states of every chunk, twice, and two rows a sample
     assert back(0, 1, 320, 1, 1, 64, 64) >= 4 * (2 * 10 * 64 * 64 + 2 * 320 * 64)
     assert back(0, 0, 320, 1, 1, 64, 64) == 0 and back(0, 1, 0, 1, 1, 64, 64) == 0
+
+
+def test_workspaces_on_16_bytes():
+    odd = ctypes.c_void_p(0x1008)
+    assert _rule(L=500, ws=odd) == spk.SPK_E_ARG and b"aligned" in spk.lib().spk_last_error()
+    assert _back(ws=odd) == spk.SPK_E_ARG and b"aligned" in spk.lib().spk_last_error()
+    assert _draw(C=50000, ws=odd) == spk.SPK_E_ARG and b"aligned" in spk.lib().spk_last_error()
+    assert _draw(C=50000, n=64) == spk.SPK_E_WORKSPACE
+    assert spk.spk_sample_winners_workspace_size(0, 2, 10, 1, 1) == 0
+    assert 0 < spk.spk_sample_winners_workspace_size(0, 2, 50000, 1, 1) < spk.spk_sample_winners_workspace_size(
+        0, 4, 50000, 1, 1)
+
+
+def test_large_counts_are_refused():
+    assert _draw(B=(1 << 21) + 1) == spk.SPK_E_RANGE
+    assert _draw(B=65536, C=16385) == spk.SPK_E_RANGE
+    assert _rule(B=1, Hk=1, Hv=2048, dv=4096) == spk.SPK_E_RANGE  # rows of more than 2^22 values
