@@ -83,40 +83,44 @@ __device__ __forceinline__ void tri_at(int f, int *mt, int *gp) {
 }
 
 // LDS of the operand kernel: the fragments of K and Q, whose room A and T take
-// once the products are made; then the products K K^T and Q K^T.
+// once the products are made (and, before T, P).
 template <class E, int DS>
 struct PrepLds {
     using B = Lay<E, DS>;
     static constexpr int PITCH = B::C + 4;  // floats; 16-byte rows, four banks on from row to row
     static constexpr int SQ = B::C * PITCH * 4;
     static constexpr int R0 = 2 * B::K > 2 * SQ ? 2 * B::K : 2 * SQ;
-    static constexpr int BYTES = R0 + 2 * SQ + B::C * 8 + B::C * 4;
+    static constexpr int HEADS = PREP_THREADS / 64;  // whose decays are made at a time
+    static constexpr int BYTES = R0 + HEADS * B::C * 12;
 };
 
 // Grid (chunk, b * Hk + key head): the fragments of the chunk's keys and
 // queries, their products, and for each value head of the key head T, P and the
-// coefficients.  T by blocks of 16: the diagonal ones by substitution, a column
-// a lane; the rest of block column j by
+// coefficients.  The products stay in registers, a row of tiles a wave.  T by
+// blocks of 16: the diagonal ones by substitution, a column a lane; the rest of
+// block column j by
 //     T_ij = -T_ii sum over j <= m < i of A_im T_mj
-// on the float matrix cores, a block column a wave.
+// on the float matrix cores, a block column a wave.  The steps are short and
+// wait for each other, so the LDS is kept small enough for four workgroups a CU
+// (dk <= 128, bfloat16).
 template <class E, int DS, bool BWD>
-__global__ __launch_bounds__(PREP_THREADS) void k_delta_prep(const E *__restrict__ q, const E *__restrict__ k,
-                                                             const float *__restrict__ g,
-                                                             const float *__restrict__ beta, Args a,
-                                                             const int32_t *__restrict__ lengths, int wide, Chunks w) {
+__global__ __launch_bounds__(PREP_THREADS, 4) void k_delta_prep(const E *__restrict__ q, const E *__restrict__ k,
+                                                                const float *__restrict__ g,
+                                                                const float *__restrict__ beta, Args a,
+                                                                const int32_t *__restrict__ lengths, int wide, Chunks w) {
     using F = Blob<E, DS, BWD>;
     using S = PrepLds<E, DS>;
     constexpr int C = F::C, MT = F::MT, NT = F::NT, PITCH = S::PITCH;
     extern __shared__ char lds[];
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, m = lane & 15, gr = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, gr = lane >> 4;
+    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int chunk = blockIdx.x, b = blockIdx.y / a.Hk, hk = blockIdx.y % a.Hk, rep = a.Hv / a.Hk;
     const int n = (lengths ? max(0, min(a.L, lengths[b])) : a.L) - chunk * C;  // samples from the chunk's first on
     if (n <= 0) return;
     char *fk = lds, *fq = lds + F::K;
     float *A = reinterpret_cast<float *>(lds), *T = A + C * PITCH;
-    float *G = reinterpret_cast<float *>(lds + S::R0), *H = G + C * PITCH;
-    double *gam = reinterpret_cast<double *>(lds + S::R0 + 2 * S::SQ);
-    float *bet = reinterpret_cast<float *>(gam + C);
+    double *gam = reinterpret_cast<double *>(lds + S::R0);      // [HEADS][C]
+    float *bet = reinterpret_cast<float *>(gam + S::HEADS * C);  // [HEADS][C]
     char *key = w.key + ((int64_t)blockIdx.y * w.NC + chunk) * F::KEY;
 
     // K and Q: four units of a thread at a time, so that their loads overlap
@@ -147,51 +151,74 @@ __global__ __launch_bounds__(PREP_THREADS) void k_delta_prep(const E *__restrict
     if (wide) units(std::true_type{});
     else units(std::false_type{});
     __syncthreads();
-    // lower tiles of K K^T (rows 0..MT-1 of the list) and Q K^T (the rest, from the last row on)
-    for (int row = wv; row < 2 * MT; row += PREP_THREADS / 64) {
-        const bool isq = row >= MT;
-        const int mt = isq ? 2 * MT - 1 - row : row;
-        const char *fa = isq ? fq : fk;
-        for (int nt = 0; nt <= mt; ++nt) {
-            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    // lower tiles of K K^T (row wv) and Q K^T (row 3 - wv), where there are such rows
+    const int grow = wv, hrow = 3 - wv;
+    f32x4 G[MT], H[MT];
 #pragma unroll
-            for (int s = 0; s < DS; ++s)
-                mma<NT, NT>(acc, frag<NT>(fa + (mt * DS + s) * NT * FRAG, lane),
+    for (int nt = 0; nt < MT; ++nt) {
+        G[nt] = H[nt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < DS; ++s) {
+            if (nt <= grow && grow < MT)
+                mma<NT, NT>(G[nt], frag<NT>(fk + (grow * DS + s) * NT * FRAG, lane),
                             frag<NT>(fk + (nt * DS + s) * NT * FRAG, lane));
-#pragma unroll
-            for (int r = 0; r < 4; ++r) (isq ? H : G)[(16 * mt + 4 * gr + r) * PITCH + 16 * nt + m] = acc[r];
+            if (nt <= hrow && hrow < MT)
+                mma<NT, NT>(H[nt], frag<NT>(fq + (hrow * DS + s) * NT * FRAG, lane),
+                            frag<NT>(fk + (nt * DS + s) * NT * FRAG, lane));
         }
     }
-    __syncthreads();  // the fragments' room is free
     for (int hr = 0; hr < rep; ++hr) {
-        const int h = hk * rep + hr;
-        char *head = w.head + (((int64_t)b * a.Hv + h) * w.NC + chunk) * F::HEAD;
-        if (tid < 64) {
-            const int64_t at = ((int64_t)b * a.L + chunk * C + tid) * a.Hv + h;
-            const bool in = tid < C && tid < n;
-            double s = in ? log_decay(g[at]) : 0.0;
+        const int hs = hr % S::HEADS;
+        char *head = w.head + (((int64_t)b * a.Hv + hk * rep + hr) * w.NC + chunk) * F::HEAD;
+        if (hs == 0) {  // the decays of the next heads, one a wave
+            const int h = hk * rep + hr + wv;
+            if (hr + wv < rep) {
+                const int64_t at = ((int64_t)b * a.L + chunk * C + min(lane, n - 1)) * a.Hv + h;
+                const bool in = lane < C && lane < n;
+                const float gv = g[at], bv = beta[at];
+                double s = in ? log_decay(gv) : 0.0;
 #pragma unroll
-            for (int o = 1; o < C; o <<= 1) {
-                const double p = __shfl_up(s, o, 64);
-                if (tid >= o) s += p;
+                for (int o = 1; o < C; o <<= 1) {
+                    const double p = __shfl_up(s, o, 64);
+                    if (lane >= o) s += p;
+                }
+                const double end = __shfl(s, C - 1, 64);
+                if (lane < C) {
+                    gam[wv * C + lane] = s;
+                    bet[wv * C + lane] = in ? bv : 0.0f;
+                    float *co = reinterpret_cast<float *>(w.head + (((int64_t)b * a.Hv + h) * w.NC + chunk) * F::HEAD + F::T);
+                    const float e = expf((float)s);
+                    co[lane] = e;
+                    co[C + lane] = in ? bv : 0.0f;
+                    co[2 * C + lane] = expf((float)(end - s));
+                    co[3 * C + lane] = a.scale * e;
+                }
             }
-            const double end = __shfl(s, C - 1, 64);
-            if (tid < C) {
-                const float be = in ? beta[at] : 0.0f;
-                gam[tid] = s;
-                bet[tid] = be;
-                float *co = reinterpret_cast<float *>(head + F::T);
-                co[tid] = expf((float)s);
-                co[C + tid] = be;
-                co[2 * C + tid] = expf((float)(end - s));
-                co[3 * C + tid] = a.scale * expf((float)s);
+        }
+        __syncthreads();  // (the fragments', or the last head's, room is free)
+        const double *gm = gam + hs * C;
+        const float *bt = bet + hs * C;
+        // A, and P in T's room
+#pragma unroll
+        for (int nt = 0; nt < MT; ++nt) {
+            const int j = 16 * nt + m;
+            const double gj = gm[j];
+            if (nt <= grow && grow < MT) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = 16 * grow + 4 * gr + r;
+                    A[i * PITCH + j] = bt[i] * expf((float)(j < i ? gm[i] - gj : 0.0)) * G[nt][r];
+                }
+            }
+            if (nt <= hrow && hrow < MT) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = 16 * hrow + 4 * gr + r;
+                    T[i * PITCH + j] = j <= i ? a.scale * expf((float)(j < i ? gm[i] - gj : 0.0)) * H[nt][r] : 0.0f;
+                }
             }
         }
         __syncthreads();
-        for (int e = tid; e < C * C; e += PREP_THREADS) {
-            const int i = e / C, j = e % C;
-            if (j < i) A[i * PITCH + j] = bet[i] * expf((float)(gam[i] - gam[j])) * G[i * PITCH + j];
-        }
         for (int u = tid; u < F::TRI * 64; u += PREP_THREADS) {  // P, or P^T
             const int f = u >> 6;
             int mt, gp;
@@ -201,14 +228,14 @@ __global__ __launch_bounds__(PREP_THREADS) void k_delta_prep(const E *__restrict
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int c = 32 * gp + slot(gr, j), lo = BWD ? i : c, hi = BWD ? c : i;
-                x[j] = lo <= hi ? a.scale * expf((float)(gam[hi] - gam[lo])) * H[hi * PITCH + lo] : 0.0f;
+                const float p = T[hi * PITCH + lo];
+                x[j] = lo <= hi ? p : 0.0f;
             }
             put_frag<F::NP>(head + F::PAT + f * F::NP * FRAG, lane, split<F::NP>(x));
         }
-        __syncthreads();
+        float x[16];
         if (wv < MT) {  // diagonal block wv, column m (all lane groups alike)
             const float *Ab = A + 16 * wv * PITCH + 16 * wv;
-            float x[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 float s = i == m ? 1.0f : 0.0f;
@@ -216,10 +243,11 @@ __global__ __launch_bounds__(PREP_THREADS) void k_delta_prep(const E *__restrict
                 for (int j = 0; j < i; ++j) s -= Ab[i * PITCH + j] * x[j];
                 x[i] = s;
             }
-            if (gr == 0) {
+        }
+        __syncthreads();
+        if (wv < MT && gr == 0) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) T[(16 * wv + i) * PITCH + 16 * wv + m] = x[i];
-            }
+            for (int i = 0; i < 16; ++i) T[(16 * wv + i) * PITCH + 16 * wv + m] = x[i];
         }
         __syncthreads();
         if (wv < MT - 1) {  // block column wv
@@ -256,15 +284,16 @@ __global__ __launch_bounds__(PREP_THREADS) void k_delta_prep(const E *__restrict
             if (up) tri_at<MT, true>(f, &mt, &gp);
             else tri_at<MT, false>(f, &mt, &gp);
             const int i = 16 * mt + m;
-            float x[8];
+            float y[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int c = 32 * gp + slot(gr, j), lo = up ? i : c, hi = up ? c : i;
-                x[j] = lo <= hi ? T[hi * PITCH + lo] : 0.0f;
+                const float t = T[hi * PITCH + lo];
+                y[j] = lo <= hi ? t : 0.0f;
             }
-            put_frag<3>(head + (up ? F::TTAT : 0) + f * 3 * FRAG, lane, split<3>(x));
+            put_frag<3>(head + (up ? F::TTAT : 0) + f * 3 * FRAG, lane, split<3>(y));
         }
-        __syncthreads();
+        if (hr + 1 < rep) __syncthreads();
     }
 }
 
