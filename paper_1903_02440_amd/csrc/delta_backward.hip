@@ -30,7 +30,7 @@ template <class E, int DS, int KS>
 struct RscanLds {
     using F = Blob<E, DS, true>;
     static constexpr int TP = F::HEAD - F::T;  // coefficients, T^T, P^T
-    static constexpr int X = KS > 1 ? 8 * F::MT * FRAG : 0;
+    static constexpr int X = KS > 1 ? carriers<DS, KS>() * F::MT * FRAG : 0;
     static constexpr int KB = 3 * F::K + TP + X <= LDS_BYTES ? 2 : 1;
     static constexpr int AT_Q = KB * F::K, AT_TP = AT_Q + F::K, AT_X = AT_TP + TP, BYTES = AT_X + X;
     static_assert(BYTES <= LDS_BYTES, "LDS");
@@ -626,7 +626,7 @@ void launch_rscan(const Cols &cols, const E *d_out, const Args &a, const int32_t
                   const Kept &kept, const float *d_last, float *d_first, hipStream_t st) {
     constexpr int LDS = RscanLds<E, DS, KS>::BYTES;
     hipLaunchKernelGGL((k_delta_rscan<E, DS, KS>), dim3((unsigned)(a.B * a.Hv), (unsigned)cols.blocks),
-                       dim3((unsigned)cols.threads), LDS, st, d_out, a, lengths, cols.tiles, w, kept, d_last, d_first);
+                       dim3(64 * std::max(4, cols.tiles * KS)), LDS, st, d_out, a, lengths, cols.tiles, w, kept, d_last, d_first);
 }
 
 struct Call {

@@ -301,18 +301,33 @@ __global__ __launch_bounds__(PREP_THREADS, 4) void k_delta_prep(const E *__restr
 // key head, which read the same operands, on one XCD's L2.
 __device__ __forceinline__ int head_of(int x, int n) { return n % 8 == 0 ? (x & 7) * (n >> 3) + (x >> 3) : x; }
 
-// LDS of the states' kernel, for KS waves to a tile of 16 columns and at most
-// eight in all.  K is needed all through a chunk and has two buffers where they
+// Waves of a workgroup that only copy the next chunk's operands to LDS.  The
+// copies go out at some 64 bytes a cycle and CU, and a wave that issues them
+// waits for that (2400 of 7100 cycles of a chunk of 250x10 memories, float, and
+// as much of 11000 of 128x128 ones, bfloat16).
+constexpr int COPIERS = 4;
+
+// Waves that carry columns, at most: those of one kernel are limited by their
+// registers.
+template <int DS, int KS>
+constexpr int carriers() {
+    return DS == 8 && KS == 1 ? 4 : 8;
+}
+
+// LDS of the states' kernel, for KS waves to a tile of 16 columns.  K is needed all through a chunk and has two buffers where they
 // fit; T, the coefficients and P from the middle on, with two where those still
-// fit; Q is done with in the middle and has one.  Then the partial sums that the
-// waves of a tile exchange.
+// fit; Q is done with in the middle and has one, or none (DIRECT) where K's second
+// only fits without it and a wave has registers for its own part of Q.  Then the
+// partial sums that the waves of a tile exchange.
 template <class E, int DS, int KS, bool STATES>
 struct ScanLds {
     using F = Blob<E, DS, STATES>;
-    static constexpr int Q = STATES ? 0 : F::K, TP = STATES ? F::T + F::COEF : F::HEAD;
-    static constexpr int TILES = 8 / KS;
-    static constexpr int X = KS > 1 ? 8 * F::MT * FRAG : 0;
+    static constexpr int TP = STATES ? F::T + F::COEF : F::HEAD, TILES = carriers<DS, KS>() / KS;
+    static constexpr int X = KS > 1 ? carriers<DS, KS>() * F::MT * FRAG : 0;
     static constexpr int Y = STATES ? 0 : TILES * F::MT * (KS - 1) * FRAG;
+    static constexpr bool DIRECT = !STATES && F::MT * (DS / KS) * F::NT <= 12 && 3 * F::K + TP + X + Y > LDS_BYTES &&
+                                   2 * F::K + TP + X + Y <= LDS_BYTES;
+    static constexpr int Q = STATES || DIRECT ? 0 : F::K;
     static constexpr int KB = 2 * F::K + Q + TP + X + Y <= LDS_BYTES ? 2 : 1;
     static constexpr int TB = KB * F::K + Q + 2 * TP + X + Y <= LDS_BYTES ? 2 : 1;
     static constexpr int AT_Q = KB * F::K, AT_TP = AT_Q + Q, AT_X = AT_TP + TB * TP, AT_Y = AT_X + X,
@@ -325,11 +340,10 @@ struct ScanLds {
 // registers: as the right operand of K S and Q S (three terms) and as the sums of
 // K^T (last U).  They add up K S through LDS in the middle of a chunk, after
 // which each has U for itself; of out each finishes some rows.  KS = 1 where the
-// columns alone fill the SIMDs, more where they do not.  Waves without columns
-// help to copy.  STATES: for the backward pass, the state that enters each chunk
+// columns alone fill the SIMDs, more where they do not.  STATES: for the backward pass, the state that enters each chunk
 // and U are written instead of out (`kept`).
 template <class E, int DS, int KS, bool STATES>
-__global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Args a,
+__global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_scan(const E *__restrict__ v, Args a,
                                                     const int32_t *__restrict__ lengths, int tiles, Chunks w,
                                                     const float *state_in, E *__restrict__ out, float *state_out,
                                                     Kept kept) {
@@ -338,7 +352,7 @@ __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Arg
     constexpr int C = F::C, MT = F::MT, NT = F::NT, GP = F::GP, NP = F::NP, DW = DS / KS;
     extern __shared__ char lds[];
     const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, gr = lane >> 4;
-    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), cw = wv - tiles * KS;  // cw >= 0: a copier
     const int tile = wv / KS, part = wv % KS, s0 = part * DW;  // the wave's columns and groups of dk
     const int bh = head_of(blockIdx.x, gridDim.x), b = bh / a.Hv, h = bh % a.Hv, hk = h / (a.Hv / a.Hk);
     const int n = lengths ? max(0, min(a.L, lengths[b])) : a.L, nc = (n + C - 1) / C;
@@ -360,12 +374,12 @@ __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Arg
 #pragma unroll
             for (int r = 0; r < 4; ++r) S[t][r] = live && dk_of(2 * s0 + t, 4 * gr + r) < a.dk ? S[t][r] : 0.0f;
     }
-    auto fetch_k = [&](int c) { to_lds(lds + (c % M::KB) * F::K, key + (int64_t)c * F::KEY, F::K, wv, waves, lane); };
+    auto fetch_k = [&](int c) { to_lds(lds + (c % M::KB) * F::K, key + (int64_t)c * F::KEY, F::K, cw, COPIERS, lane); };
     auto fetch_q = [&](int c) {
-        if (!STATES) to_lds(lds + M::AT_Q, key + (int64_t)c * F::KEY + F::K, F::K, wv, waves, lane);
+        if (M::Q) to_lds(lds + M::AT_Q, key + (int64_t)c * F::KEY + F::K, F::K, cw, COPIERS, lane);
     };
     auto fetch_t = [&](int c) {
-        to_lds(lds + M::AT_TP + (c % M::TB) * M::TP, head + (int64_t)c * F::HEAD, M::TP, wv, waves, lane);
+        to_lds(lds + M::AT_TP + (c % M::TB) * M::TP, head + (int64_t)c * F::HEAD, M::TP, cw, COPIERS, lane);
     };
     // sample i of the chunk, column col: uniform rows and the lane's offset within four of them
     const int64_t vstep = (int64_t)a.Hv * a.dv;
@@ -392,11 +406,25 @@ __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Arg
                     vv[mt][r] = p[min(16 * mt + 4 * gr + r, n - 1 - c * C) * vstep + min(col, a.dv - 1)];
         }
     };
+    Terms<NT> qd[M::DIRECT ? DW : 1][MT];  // the wave's part of Q
+    auto direct_q = [&](int c) {
+        if (M::DIRECT) {
+            const char *p = key + (int64_t)c * F::KEY + F::K;
+#pragma unroll
+            for (int s = 0; s < (M::DIRECT ? DW : 0); ++s)
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) qd[s][mt] = frag<NT>(p + (mt * DS + s0 + s) * NT * FRAG, lane);
+        }
+    };
     if (nc) {
-        values(0);
-        fetch_k(0);
-        fetch_q(0);
-        fetch_t(0);
+        if (cw >= 0) {
+            fetch_k(0);
+            fetch_q(0);
+            fetch_t(0);
+        } else {
+            values(0);
+            direct_q(0);
+        }
         wait_copies();
     }
     __syncthreads();
@@ -405,6 +433,7 @@ __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Arg
                    *P = T + F::PAT;
         const float *co = reinterpret_cast<const float *>(T + F::T);
         f32x4 X[MT], Y[MT];
+        float vc[MT][4];
         if (mine) {
             if (STATES) {
                 float *dst = kept.S + ((int64_t)bh * w.NC + c) * 32 * DS * kept.dvp;
@@ -425,8 +454,21 @@ __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Arg
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {
                     mma<NT, 3>(X[mt], frag<NT>(K + (mt * DS + s0 + s) * NT * FRAG, lane), st);
-                    if (!STATES) mma<NT, NP>(Y[mt], frag<NT>(Q + (mt * DS + s0 + s) * NT * FRAG, lane), sp);
+                    if (M::DIRECT) mma<NT, NP>(Y[mt], qd[M::DIRECT ? s : 0][mt], sp);
+                    else if (!STATES) mma<NT, NP>(Y[mt], frag<NT>(Q + (mt * DS + s0 + s) * NT * FRAG, lane), sp);
                 }
+            }
+            // the wave's own loads go out before the copies take the CU's path to memory
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    vc[mt][r] = to_float(vv[mt][r]);
+                    if (STATES) vc[mt][r] = live ? vc[mt][r] : 0.0f;  // (the padding is read by others)
+                }
+            if (c + 1 < nc) {
+                values(c + 1);
+                direct_q(c + 1);
             }
             if (KS > 1) {
                 char *xb = lds + M::AT_X + tile * KS * MT * FRAG, *yb = lds + M::AT_Y + tile * MT * (KS - 1) * FRAG;
@@ -441,16 +483,7 @@ __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Arg
         }
         if (M::TB == 1) wait_copies();  // (T and P of this chunk)
         lds_barrier();
-        float vc[MT][4];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                vc[mt][r] = to_float(vv[mt][r]);
-                if (STATES) vc[mt][r] = live ? vc[mt][r] : 0.0f;  // (the padding is read by others)
-            }
-        if (c + 1 < nc) {
-            values(c + 1);
+        if (c + 1 < nc && cw >= 0) {
             fetch_q(c + 1);
             if (M::KB == 2) fetch_k(c + 1);
             if (M::TB == 2) fetch_t(c + 1);
@@ -518,7 +551,7 @@ __global__ __launch_bounds__(512) void k_delta_scan(const E *__restrict__ v, Arg
         // the next chunk's operands have come; what is stored now has half a chunk's time to get out
         wait_copies();
         lds_barrier();
-        if (c + 1 < nc) {
+        if (c + 1 < nc && cw >= 0) {
             if (M::KB == 1) fetch_k(c + 1);
             if (M::TB == 1) fetch_t(c + 1);
         }
@@ -571,11 +604,12 @@ inline Cols columns(const Args &a, int all, int DS) {
     Cols c;
     const int64_t waves = (int64_t)a.B * a.Hv * all;
     c.KS = 1;
-    while (c.KS < 4 && 2 * c.KS <= DS && waves * c.KS <= 1024) c.KS *= 2;  // up to two waves on each of 1024 SIMDs
-    c.tiles = all < 8 / c.KS ? all : 8 / c.KS;
+    while (c.KS < 8 && 2 * c.KS <= DS && waves * c.KS <= 1024) c.KS *= 2;  // up to two waves on each of 1024 SIMDs
+    const int most = (DS == 8 && c.KS == 1 ? 4 : 8) / c.KS;
+    c.tiles = all < most ? all : most;
     while (c.tiles > 1 && (int64_t)a.B * a.Hv * ((all + c.tiles - 1) / c.tiles) < 256) c.tiles = (c.tiles + 1) / 2;
     c.blocks = (all + c.tiles - 1) / c.tiles;
-    c.threads = 64 * (c.tiles * c.KS > 4 ? c.tiles * c.KS : 4);
+    c.threads = 64 * (c.tiles * c.KS + COPIERS);
     return c;
 }
 
@@ -589,7 +623,9 @@ void launch_scan(const Cols &cols, const void *v, const Args &a, const int32_t *
 }
 // CALL(KS) with the form that `cols` asks for
 #define SPK_DELTA_PARTS(DS, cols, CALL)      \
-    if (DS >= 4 && (cols).KS == 4) {         \
+    if (DS >= 8 && (cols).KS == 8) {         \
+        CALL((DS >= 8 ? 8 : 1));             \
+    } else if (DS >= 4 && (cols).KS == 4) {  \
         CALL((DS >= 4 ? 4 : 1));             \
     } else if (DS >= 2 && (cols).KS == 2) {  \
         CALL((DS >= 2 ? 2 : 1));             \
