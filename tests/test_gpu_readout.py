@@ -132,7 +132,8 @@ def test_delta_rule_gates(dtype):
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("B,Hk,Hv,dk,dv", [(1, 1, 1, 1, 1), (3, 2, 4, 7, 5), (2, 1, 8, 250, 10), (4, 2, 4, 128, 128),
-                                           (1, 1, 1, 256, 300), (5, 3, 3, 100, 36), (1, 2, 2, 17, 130)])
+                                           (1, 1, 1, 256, 300), (5, 3, 3, 100, 36), (1, 2, 2, 17, 130), (2, 1, 2, 70, 129),
+                                           (1, 1, 1, 256, 3), (2, 2, 2, 30, 131), (3, 1, 1, 200, 257)])
 def test_delta_step(B, Hk, Hv, dk, dv, dtype):
     """Sample after sample with the state in place, against the batch definition."""
     L = 6
