@@ -9,8 +9,9 @@
  * host; arguments validated on the host before anything is enqueued; SPK_E_*
  * statuses with spk_last_error().  Pointers need the alignment of their
  * element only; 16-byte aligned ones (and row lengths that are multiples of
- * 16 bytes) take wider loads.  A workspace must be 16-byte aligned.  Outputs
- * must not overlap inputs or each other unless stated.
+ * 16 bytes) take wider loads.  A workspace must be 16-byte aligned, and calls
+ * that may run at the same time need one each.  Outputs must not overlap inputs
+ * or each other unless stated.
  */
 #ifndef LIBSPYKE_READOUT_H
 #define LIBSPYKE_READOUT_H

@@ -5,9 +5,11 @@ scores.
 The functions have the names of the C entry points and, as those of the package,
 only marshal: dtype and shape checks, outputs and workspaces that are not given,
 raw pointers and the stream.  The call runs on the tensors' device, on its
-current stream unless one is given.
+current stream unless one is given (keyword ``stream``).
 """
 from __future__ import annotations
+
+import functools
 
 import torch
 
@@ -51,13 +53,27 @@ def _at(dev, name, t):
     return t.data_ptr()
 
 
-def _on(dev, stream, call):
-    """call(stream handle) with `dev` current (a launch goes to the current device)."""
+def _on(dev, call):
+    """call(stream handle) on the current stream of `dev`, with `dev` current (a launch goes to the current device)."""
     if dev.index == torch.cuda.current_device():
-        _check(call(stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(dev.index)))
+        _check(call(torch._C._cuda_getCurrentRawStream(dev.index)))
         return
     with torch.cuda.device(dev):
-        _check(call(stream.cuda_stream if stream is not None else torch.cuda.current_stream(dev).cuda_stream))
+        _check(call(torch.cuda.current_stream(dev).cuda_stream))
+
+
+def _with_stream(fn):
+    """Adds the keyword `stream`: the call runs with it current, so that outputs and workspaces made here are its too."""
+    @functools.wraps(fn)
+    def call(*args, stream=None, **kw):
+        if stream is None:
+            return fn(*args, **kw)
+        for t in (*args, *kw.values()):
+            if isinstance(t, torch.Tensor) and t.device != stream.device:
+                raise ValueError(f"stream on {stream.device}, a tensor of the call on {t.device}")
+        with torch.cuda.stream(stream):
+            return fn(*args, **kw)
+    return call
 
 
 # ---------------------------------------------------------------- delta rule
@@ -96,8 +112,9 @@ def _rows(t, like, dtype, lengths, name):
     return _out(t, like.shape, dtype, like.device, name)
 
 
+@_with_stream
 def spk_delta_rule(q, k, v, g, beta, scale=1.0, initial_state=None, lengths=None, out=None, final_state=None,
-                   workspace=None, stream=None):
+                   workspace=None):
     """Gated delta rule over a batch of sequences: q, k [B,L,Hk,dk] and v [B,L,Hv,dv] of one dtype (float32 or
     bfloat16), g, beta f32 [B,L,Hv] -> (out [B,L,Hv,dv], final_state f32 [B,Hv,dk,dv] or None).  lengths i32 [B]
     gives each sequence's samples; rows of a given `out` behind them are left as they were, those of a new one
@@ -111,11 +128,12 @@ def spk_delta_rule(q, k, v, g, beta, scale=1.0, initial_state=None, lengths=None
     args = (_at(dev, "q", q), _at(dev, "k", k), _at(dev, "v", v), _at(dev, "g", g), _at(dev, "beta", beta), dt, B, L,
             Hk, Hv, dk, dv, scale, _at(dev, "lengths", lengths), _at(dev, "initial_state", initial_state),
             _at(dev, "out", out), _at(dev, "final_state", final_state), _at(dev, "workspace", ws), n)
-    _on(dev, stream, lambda st: _lib.spk_delta_rule(*args, st))
+    _on(dev, lambda st: _lib.spk_delta_rule(*args, st))
     return out, (final_state if final_state is not False else None)
 
 
-def spk_delta_rule_step(q, k, v, g, beta, state, scale=1.0, out=None, stream=None):
+@_with_stream
+def spk_delta_rule_step(q, k, v, g, beta, state, scale=1.0, out=None):
     """One sample of every sequence: q, k [B,Hk,dk], v [B,Hv,dv], g, beta f32 [B,Hv]; state f32 [B,Hv,dk,dv] is
     updated in place -> out [B,Hv,dv]."""
     for name, t in (("q", q), ("k", k), ("v", v)):
@@ -134,13 +152,13 @@ def spk_delta_rule_step(q, k, v, g, beta, state, scale=1.0, out=None, stream=Non
     out = _out(out, (B, Hv, dv), q.dtype, dev, "out")
     args = (_at(dev, "q", q), _at(dev, "k", k), _at(dev, "v", v), _at(dev, "g", g), _at(dev, "beta", beta), dt, B, Hk,
             Hv, dk, dv, scale, _at(dev, "state", state), _at(dev, "out", out))
-    _on(dev, stream, lambda st: _lib.spk_delta_rule_step(*args, st))
+    _on(dev, lambda st: _lib.spk_delta_rule_step(*args, st))
     return out
 
 
+@_with_stream
 def spk_delta_rule_backward(q, k, v, g, beta, d_out, d_final_state=None, scale=1.0, initial_state=None, lengths=None,
-                            d_q=None, d_k=None, d_v=None, d_g=None, d_beta=None, d_initial_state=None, workspace=None,
-                            stream=None):
+                            d_q=None, d_k=None, d_v=None, d_g=None, d_beta=None, d_initial_state=None, workspace=None):
     """Gradients of spk_delta_rule's (out, final_state) -> (d_q, d_k, d_v, d_g, d_beta, d_initial_state or None)
     from d_out [B,L,Hv,dv] and d_final_state f32 [B,Hv,dk,dv] (None: zeros).  Rows behind a sequence's length as in
     spk_delta_rule.  d_initial_state may be d_final_state."""
@@ -162,7 +180,7 @@ def spk_delta_rule_backward(q, k, v, g, beta, d_out, d_final_state=None, scale=1
             _at(dev, "d_out", d_out), _at(dev, "d_final_state", d_final_state), _at(dev, "d_q", d_q),
             _at(dev, "d_k", d_k), _at(dev, "d_v", d_v), _at(dev, "d_g", d_g), _at(dev, "d_beta", d_beta),
             _at(dev, "d_initial_state", d_initial_state), _at(dev, "workspace", ws), n)
-    _on(dev, stream, lambda st: _lib.spk_delta_rule_backward(*args, st))
+    _on(dev, lambda st: _lib.spk_delta_rule_backward(*args, st))
     return d_q, d_k, d_v, d_g, d_beta, (d_initial_state if d_initial_state is not False else None)
 
 
@@ -171,8 +189,9 @@ def spk_sample_winners_workspace_size(dtype, B, C, H, W) -> int:
     return int(_lib.spk_sample_winners_workspace_size(dtype, B, C, H, W))
 
 
+@_with_stream
 def spk_sample_winners(scores, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, t_first=None, T=1, winners=None,
-                       n_winners=None, workspace=None, stream=None):
+                       n_winners=None, workspace=None):
     """One winner per image drawn from scores (float32 or bfloat16) [B,C,H,W] with u f32 [B] in [0, 1) ->
     (winners i32 [B,1,4] = (f,t,y,x), n_winners i32 [B]).  t_first u8 [B,C,H,W] masks the silent neurons
     (t_first >= T)."""
@@ -192,5 +211,5 @@ def spk_sample_winners(scores, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0
     args = (_at(dev, "scores", scores), dt, _at(dev, "t_first", t_first), _at(dev, "u", u), B, T, C, H, W, temperature,
             top_k, top_p, min_p, _at(dev, "winners", winners), _at(dev, "n_winners", n_winners),
             _at(dev, "workspace", ws), n)
-    _on(dev, stream, lambda st: _lib.spk_sample_winners(*args, st))
+    _on(dev, lambda st: _lib.spk_sample_winners(*args, st))
     return winners, n_winners

@@ -134,3 +134,17 @@ def test_readout_calls_on_two_streams():
     torch.cuda.synchronize()
     for (o, l), (out, last, _) in zip(want, got):
         assert torch.equal(o, out) and torch.equal(l, last)
+
+
+def test_readout_calls_on_a_given_stream_make_their_buffers_there():
+    """Outputs and workspaces made by calls on side streams are not handed to other work while those run."""
+    x, s0 = make(2, 300, 2, 4, 64, 48, F32, 81)
+    want = spk.spk_delta_rule(**x, initial_state=s0)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for _ in range(4):
+        got = [spk.spk_delta_rule(**x, initial_state=s0, stream=st) for st in streams]
+        noise = [torch.full_like(want[0], 7.0) for _ in range(4)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, want[0]) and torch.equal(l, want[1]) for o, l in got)
+        assert all(bool((t == 7.0).all()) for t in noise)

@@ -166,3 +166,13 @@ def test_large_counts_are_refused():
     assert _draw(B=(1 << 21) + 1) == spk.SPK_E_RANGE
     assert _draw(B=65536, C=16385) == spk.SPK_E_RANGE
     assert _rule(B=1, Hk=1, Hv=2048, dv=4096) == spk.SPK_E_RANGE  # rows of more than 2^22 values
+
+
+def test_stream_of_another_device_is_refused():
+    class Other:
+        device = torch.device("cuda", 1)
+    z = torch.zeros
+    with pytest.raises(ValueError, match="stream on cuda:1"):
+        spk.spk_sample_winners(z(2, 3, 1, 1), z(2), stream=Other)
+    with pytest.raises(ValueError, match="stream on cuda:1"):
+        spk.spk_delta_rule(q=z(2, 3, 1, 4), k=z(2, 3, 1, 4), v=z(2, 3, 1, 4), g=z(2, 3, 1), beta=z(2, 3, 1), stream=Other)
