@@ -544,12 +544,15 @@ struct RowEdge {
 struct Work {
     int splits;
     uint64_t *hist;   // [B][BINS]
-    uint32_t *list;   // [B][LIST]
+    uint64_t *list;   // [B][LIST], entries
     uint32_t *count;  // [B]
     RowPart *part;    // [B][splits]
     RowSums *sums;    // [B][splits][LONG_WAVES]
     RowEdge *edge;    // [B]
 };
+
+// A score in a list: larger where it comes earlier in the order.
+__device__ __forceinline__ uint64_t entry(uint32_t key, int64_t i) { return ((uint64_t)key << 32) | (uint32_t)~(uint32_t)i; }
 
 // A long row's scores and the workgroup's share of them.
 template <class E>
@@ -569,6 +572,14 @@ struct LongRow {
     __device__ __forceinline__ void own(F f) const { for_row<E>(x, tf, T, i0, i1, threadIdx.x, LONG_THREADS, f); }
     template <class F>
     __device__ __forceinline__ void all(F f) const { for_row<E>(x, tf, T, 0, N, threadIdx.x, LONG_THREADS, f); }
+    // f(key, value()) for the row's keys from the edge up
+    template <class F, class Value>
+    __device__ __forceinline__ void each_from(const Edge &from, F f, Value value) const {
+        all([&](float v, int64_t) {
+            const uint32_t k = key_of(v);
+            if (k >= from.edge && k != 0) f(k, [&] { return value(k); });
+        });
+    }
 };
 
 // What a row's parts add up to, and the bins of its histogram.
@@ -666,12 +677,13 @@ __device__ __forceinline__ int boundary_bin(Shared<LONG_WAVES> &sh, const Sample
     return (int)find_bin<BINS, LONG_WAVES>(sh, *want, over);
 }
 
-// The keys of the boundary's bin; with COUNT those of the bins before it too, so
-// that what step 1 keeps is all there.
+// The entries of the boundary's bin; with COUNT those of the bins before it too,
+// so that what step 1 keeps is all there.
 template <class E, bool COUNT>
 __global__ __launch_bounds__(LONG_THREADS) void k_sample_list(const E *__restrict__ scores,
                                                               const uint8_t *__restrict__ t_first, SampleArgs a, Work w) {
     __shared__ Shared<LONG_WAVES> sh;
+    __shared__ uint64_t list[LIST];
     const int64_t b = blockIdx.y;
     const RowStat st(w.part + b * w.splits, w.splits, a.temperature);
     if (st.n == 0) return;
@@ -680,12 +692,12 @@ __global__ __launch_bounds__(LONG_THREADS) void k_sample_list(const E *__restric
     const LongRow<E> row(scores, t_first, a, w.splits, b, blockIdx.x);
     if (threadIdx.x == 0) sh.n_list = 0;
     __syncthreads();
-    row.own([&](float v, int64_t) {
+    row.own([&](float v, int64_t i) {
         if (!wins(v)) return;
         const int at_bin = st.bin(v);
         if (at_bin == bin || (COUNT && at_bin < bin)) {
             const uint32_t at = atomicAdd(&sh.n_list, 1u);
-            if (at < LIST) sh.list[at] = key_of(v);
+            if (at < LIST) list[at] = entry(key_of(v), i);
         }
     });
     __syncthreads();
@@ -693,7 +705,47 @@ __global__ __launch_bounds__(LONG_THREADS) void k_sample_list(const E *__restric
     if (threadIdx.x == 0) sh.bin = n ? atomicAdd(&w.count[b], n) : 0;
     __syncthreads();
     for (uint32_t i = threadIdx.x, at = sh.bin; i < n && i < LIST; i += LONG_THREADS)
-        if (at + i < LIST) w.list[b * LIST + at + i] = sh.list[i];
+        if (at + i < LIST) w.list[b * LIST + at + i] = list[i];
+}
+
+// The smallest score that can weigh min_w (some lower ones pass too).
+__device__ __forceinline__ float least(const SampleArgs &a, float top, uint64_t min_w) {
+    if (min_w <= 1) return -INFINITY;
+    const double d = (double)a.temperature * (log(ldexp((double)(min_w - 1), -a.shift)) - 1e-6);  // (at most 0)
+    const double v = (double)top + d;
+    return nextafterf((float)v, -INFINITY);
+}
+
+// Step 1's boundary, then step 2's, among the keys that each(e, f, value) calls
+// f(key, value()) with, those from the edge e up; the `n` of the list, if they are
+// few, lie in sh.list.
+template <class Each>
+__device__ __forceinline__ Edge edge_of_count(Shared<LONG_WAVES> &sh, const SampleArgs &a, const Weigher &weigh, uint32_t n,
+                                              uint32_t total, Each each) {
+    constexpr int WAVES = LONG_WAVES;
+    auto one = [](uint32_t) { return (uint64_t)1; };
+    Edge e;
+    uint64_t above;
+    if ((uint64_t)a.top_k < total) {
+        const uint32_t k = n <= 64 ? few<WAVES>(sh, n, e.edge, (uint64_t)a.top_k, one, &above)
+                                   : descend<WAVES>(sh, (uint64_t)a.top_k, [&](auto f) { each(e, f, one); }, &above);
+        e.equal = (uint64_t)a.top_k - above;
+        e.edge = k;
+    }
+    if (a.top_p < 1.0f) {
+        uint64_t sum = 0;
+        each(e, [&](uint32_t k, auto value) {
+            if (k > e.edge || e.equal == ~0ull) sum += value();
+        }, weigh);
+        sum = block_sum<WAVES>(sh, sum);
+        if (e.equal != ~0ull) sum += e.equal * weigh(e.edge);
+        const uint64_t want = share(a.top_p, sum);
+        // (the edge takes part with all its equals: one that step 1 cut has its own limit)
+        const uint32_t k = n <= 64 ? few<WAVES>(sh, n, e.edge, want, weigh, &above)
+                                   : descend<WAVES>(sh, want, [&](auto f) { each(e, f, weigh); }, &above);
+        e.by_weight(k, want, above, weigh(k));
+    }
+    return e;
 }
 
 // The boundary (each workgroup of the row finds it for itself), then the sums of
@@ -727,60 +779,38 @@ __global__ __launch_bounds__(LONG_THREADS) void k_sample_sums(const E *__restric
         const uint32_t n = w.count[b];
         const bool listed = n <= LIST;
         if (listed) {
-            for (uint32_t i = tid; i < n; i += LONG_THREADS) sh.list[i] = w.list[b * LIST + i];
+            for (uint32_t i = tid; i < n; i += LONG_THREADS) sh.list[i] = (uint32_t)(w.list[b * LIST + i] >> 32);
             __syncthreads();
         }
         // f(key, value()) for the keys from the edge up: of the list, else of the whole row
-        auto each = [&](auto f, auto value) {
+        auto each = [&](const Edge &from, auto f, auto value) {
             if (listed) {
                 for (uint32_t i = tid; i < n; i += LONG_THREADS) {
                     const uint32_t k = sh.list[i];
-                    if (k >= e.edge) f(k, [&] { return value(k); });
+                    if (k >= from.edge) f(k, [&] { return value(k); });
                 }
             } else {
-                row.all([&](float v, int64_t) {
-                    const uint32_t k = key_of(v);
-                    if (k >= e.edge && k != 0) f(k, [&] { return value(k); });
-                });
+                row.each_from(from, f, value);
             }
         };
-        auto one = [](uint32_t) { return (uint64_t)1; };
         if (FORM == 1) {
             // (the list is the boundary's bin alone; the row stands for all bins)
             const uint64_t rest = listed ? want - over : want;
             const uint32_t k = n <= 64 ? few<WAVES>(sh, n, e.edge, rest, weigh, &above)
-                                       : descend<WAVES>(sh, rest, [&](auto f) { each(f, weigh); }, &above);
+                                       : descend<WAVES>(sh, rest, [&](auto f) { each(e, f, weigh); }, &above);
             e.by_weight(k, rest, above, weigh(k));
         } else {
-            if ((uint64_t)a.top_k < st.n) {
-                const uint32_t k =
-                    n <= 64 ? few<WAVES>(sh, n, e.edge, (uint64_t)a.top_k, one, &above)
-                            : descend<WAVES>(sh, (uint64_t)a.top_k, [&](auto f) { each(f, one); }, &above);
-                e.equal = (uint64_t)a.top_k - above;
-                e.edge = k;
-            }
-            if (a.top_p < 1.0f) {
-                uint64_t sum = 0;
-                each([&](uint32_t k, auto value) {
-                    if (k > e.edge || e.equal == ~0ull) sum += value();
-                }, weigh);
-                sum = block_sum<WAVES>(sh, sum);
-                if (e.equal != ~0ull) sum += e.equal * weigh(e.edge);
-                want = share(a.top_p, sum);
-                // (the edge takes part with all its equals: one that step 1 cut has its own limit)
-                const uint32_t k = n <= 64 ? few<WAVES>(sh, n, e.edge, want, weigh, &above)
-                                           : descend<WAVES>(sh, want, [&](auto f) { each(f, weigh); }, &above);
-                e.by_weight(k, want, above, weigh(k));
-            }
+            e = edge_of_count(sh, a, weigh, n, st.n, each);
         }
     }
     const uint64_t min_w = (uint64_t)ceil(ldexp((double)a.min_p, a.shift));
     const float edge = e.edge > 1 ? value_of(e.edge) : -INFINITY;  // (1: everything that can win is above)
+    const float low = least(a, st.top, min_w);
     uint64_t sum = 0;
     uint32_t eqs = 0;
     const int64_t s0 = min(row.i1, row.i0 + wv * row.seg), s1 = min(row.i1, s0 + row.seg);
     for_row<E>(row.x, row.tf, row.T, s0, s1, lane, 64, [&](float v, int64_t) {
-        if (v > edge) {
+        if (v > edge && v >= low) {
             const uint64_t x = weigh.of(v);
             sum += x >= min_w ? x : 0;
         }
@@ -847,6 +877,108 @@ __global__ __launch_bounds__(LONG_THREADS) void k_sample_pick(const E *__restric
         put_winner(winners, n_win, b, i0 + at, row.tf ? (int)row.tf[i0 + at] : 0, a);
 }
 
+// Grid: one workgroup per row, top_k at most FEW_MAX: all three steps and the draw
+// on the row's list, which as a rule holds little more than top_k entries.  Each
+// entry is compared with all: how many come before it, the weight of those, and
+// what is kept at lower indices.  Rows with more entries than a list takes (many
+// scores of one bin) are read again instead.
+constexpr int FEW_MAX = LIST / 4;
+template <class E>
+__global__ __launch_bounds__(LONG_THREADS) void k_sample_few(const E *__restrict__ scores,
+                                                             const uint8_t *__restrict__ t_first,
+                                                             const float *__restrict__ u, SampleArgs a, Work w,
+                                                             int32_t *__restrict__ winners,
+                                                             int32_t *__restrict__ n_win) {
+    constexpr int WAVES = LONG_WAVES, SLOTS = LIST / LONG_THREADS;
+    __shared__ Shared<WAVES> sh;
+    __shared__ uint64_t ent[LIST], wt[LIST];
+    const int64_t b = blockIdx.x;
+    const int tid = threadIdx.x;
+    const RowStat st(w.part + b * w.splits, w.splits, a.temperature);
+    if (st.n == 0) {  // nothing can win (uniform)
+        if (tid < 4) winners[b * 4 + tid] = -1;
+        if (tid == 0) n_win[b] = 0;
+        return;
+    }
+    const Weigher weigh = weigher<WAVES>(sh, a, key_of(st.top));
+    const uint32_t n = w.count[b];
+    const uint64_t min_w = (uint64_t)ceil(ldexp((double)a.min_p, a.shift));
+    const uint8_t *tf = t_first ? t_first + b * a.N : nullptr;
+    __syncthreads();
+    if (n <= LIST) {
+        for (uint32_t i = tid; i < n; i += LONG_THREADS) {
+            ent[i] = w.list[b * LIST + i];
+            wt[i] = weigh((uint32_t)(ent[i] >> 32));
+        }
+        __syncthreads();
+        uint64_t before[SLOTS], sum = 0;
+        bool in[SLOTS];
+#pragma unroll
+        for (int q = 0; q < SLOTS; ++q) {
+            const uint32_t i = tid + q * LONG_THREADS;
+            before[q] = 0;
+            in[q] = false;
+            if (i >= n) continue;
+            const uint64_t x = ent[i];
+            uint32_t rank = 0;
+            for (uint32_t j = 0; j < n; ++j) {
+                const bool first = ent[j] > x;
+                rank += first;
+                before[q] += first ? wt[j] : 0;
+            }
+            in[q] = rank < (uint32_t)a.top_k;
+            sum += in[q] ? wt[i] : 0;
+        }
+        sum = block_sum<WAVES>(sh, sum);
+        const uint64_t want = a.top_p < 1.0f ? share(a.top_p, sum) : ~0ull;
+        sum = 0;
+        uint64_t own[SLOTS];
+#pragma unroll
+        for (int q = 0; q < SLOTS; ++q) {
+            const uint32_t i = tid + q * LONG_THREADS;
+            own[q] = 0;
+            if (i >= n) continue;
+            if (in[q] && before[q] < want && wt[i] >= min_w) own[q] = wt[i];
+            wt[i] = own[q];  // (the weights of all were read before the sum's barriers)
+            sum += own[q];
+        }
+        const uint64_t target = target_of(u[b], block_sum<WAVES>(sh, sum));
+#pragma unroll
+        for (int q = 0; q < SLOTS; ++q) {
+            if (own[q] == 0) continue;
+            const uint32_t i = tid + q * LONG_THREADS, x = (uint32_t)ent[i];
+            uint64_t run = 0;
+            for (uint32_t j = 0; j < n; ++j) run += (uint32_t)ent[j] > x ? wt[j] : 0;  // (a lower index)
+            if (target >= run && target < run + own[q]) {
+                const int64_t at = (uint32_t)~x;
+                put_winner(winners, n_win, b, at, tf ? (int)tf[at] : 0, a);
+            }
+        }
+        return;
+    }
+    const LongRow<E> row(scores, t_first, a, 1, b, 0);
+    const Edge e = edge_of_count(sh, a, weigh, n, st.n,
+                                 [&](const Edge &from, auto f, auto value) { row.each_from(from, f, value); });
+    uint64_t we = weigh(e.edge), sum = 0, eqs = 0;
+    we = we >= min_w && e.edge > 1 ? we : 0;
+    row.all([&](float v, int64_t) {
+        const uint32_t k = key_of(v);
+        const uint64_t x = k > e.edge ? weigh(k) : 0;
+        sum += x >= min_w ? x : 0;
+        eqs += k == e.edge;
+    });
+    sum = block_sum<WAVES>(sh, sum);
+    eqs = block_sum<WAVES>(sh, eqs);
+    const uint64_t target = target_of(u[b], sum + (eqs < e.equal ? eqs : e.equal) * we);
+    const int64_t per = (a.N + LONG_THREADS - 1) / LONG_THREADS, i0 = min(a.N, tid * per), i1 = min(a.N, i0 + per);
+    int64_t at;
+    if (pick<WAVES>(sh, weigh, we, e, min_w, target, 0, 0, i1 - i0, [&](int64_t i) {
+            const uint32_t k = key_of(as_float<E>(row.x[i0 + i]));
+            return tf && tf[i0 + i] >= a.T ? 0u : k;
+        }, &at))
+        put_winner(winners, n_win, b, i0 + at, tf ? (int)tf[i0 + at] : 0, a);
+}
+
 constexpr int64_t SHORT_MAX = 16 * 64 * 16;  // keys of a row that the registers of a workgroup take
 
 // Workgroups of a long row: about two for each of 256 CUs in all, no less than
@@ -861,7 +993,7 @@ size_t carve(void *ws, int B, int64_t N, Work *w) {
     spk::Carver c(ws);
     w->splits = splits_of(B, N);
     w->hist = c.take<uint64_t>((size_t)B * BINS);
-    w->list = c.take<uint32_t>((size_t)B * LIST);
+    w->list = c.take<uint64_t>((size_t)B * LIST);
     w->count = c.take<uint32_t>(B);
     w->part = c.take<RowPart>((size_t)B * w->splits);
     w->sums = c.take<RowSums>((size_t)B * w->splits * LONG_WAVES);
@@ -890,6 +1022,10 @@ void launch(const void *scores, const uint8_t *t_first, const float *u, int B, c
     if (by_count) {
         hipLaunchKernelGGL((k_sample_hist<E, true>), grid, threads, 0, st, x, t_first, a, w);
         hipLaunchKernelGGL((k_sample_list<E, true>), grid, threads, 0, st, x, t_first, a, w);
+        if (a.top_k <= FEW_MAX) {
+            hipLaunchKernelGGL(k_sample_few<E>, rows, threads, 0, st, x, t_first, u, a, w, winners, n_winners);
+            return;
+        }
         hipLaunchKernelGGL((k_sample_sums<E, 2>), grid, threads, 0, st, x, t_first, a, w);
     } else if (!one && a.top_p < 1.0f) {
         hipLaunchKernelGGL((k_sample_hist<E, false>), grid, threads, 0, st, x, t_first, a, w);

@@ -335,3 +335,20 @@ def test_readout_learns_draws_and_rewards():
     drawn = torch.unique(lw[ln > 0][:, 0, 0]).long()
     changed = (W != 0.5).flatten(1).any(1)
     assert bool(changed[drawn].any()) and not bool(changed[[c for c in range(C) if c not in drawn.tolist()]].any())
+
+
+@pytest.mark.parametrize("top_k", [1, 2, 300, 1024, 1025, 4096])
+@pytest.mark.parametrize("steps", [1.0, 8.0, 1e6])
+def test_sample_of_long_rows_by_count(top_k, steps):
+    """Boundaries with few and many equal scores on both sides of what one list takes, and rows of few scores that
+    can win."""
+    randn, rand = seeded(top_k)
+    B, N = 4, 60001
+    x, u = (randn(B, N, 1, 1) * 2 * steps).round() / steps, rand(B)
+    x[1, 700:] = -math.inf
+    x[2, 3:] = math.nan
+    flat = torch.where(x.isnan(), -math.inf, x.double()).reshape(B, N).cuda()
+    for kw in (dict(), dict(top_p=0.75), dict(top_p=0.5, min_p=0.125), dict(min_p=0.9375), dict(min_p=2.0 ** -40)):
+        w, n = spk.spk_sample_winners(x.cuda(), u.cuda(), temperature=1.5, top_k=top_k, **kw)
+        at = in_order(flat, u.cuda(), **{"temperature": 1.5, "top_k": top_k, "top_p": 1.0, "min_p": 0.0, **kw})
+        assert torch.equal(w[:, 0, 0].long(), at) and bool((n == 1).all()), kw
