@@ -117,19 +117,22 @@ __device__ __forceinline__ uint64_t block_sum(Shared<WAVES> &sh, uint64_t v) {
 // the last one if it never does; *above gets the total of the bins before it.
 template <int N, int WAVES>
 __device__ __forceinline__ uint32_t find_bin(Shared<WAVES> &sh, uint64_t want, uint64_t *above) {
+    constexpr int THREADS = WAVES * 64, PER = N < THREADS ? 1 : N / THREADS, USED = N / PER;  // bins of a thread
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     __syncthreads();
-    if (threadIdx.x < 64) {
-        constexpr int PER = N / 64;
-        const int lane = threadIdx.x;
-        uint64_t v[PER], sum = 0;
+    uint64_t v[PER], sum = 0;
 #pragma unroll
-        for (int j = 0; j < PER; ++j) v[j] = sh.hist[lane * PER + j];
+    for (int j = 0; j < PER; ++j) {
+        v[j] = tid < USED ? sh.hist[tid * PER + j] : 0;
+        sum += v[j];
+    }
+    const uint64_t incl = wave_scan_u64(sum, lane);
+    if (lane == 63) sh.part[wv] = incl;
+    __syncthreads();
+    uint64_t run = incl - sum;
 #pragma unroll
-        for (int j = 0; j < PER; ++j) sum += v[j];
-        const uint64_t incl = wave_scan_u64(sum, lane);
-        const uint64_t hit = __ballot(incl >= want);
-        const int src = hit ? __ffsll((unsigned long long)hit) - 1 : 63;
-        uint64_t run = incl - sum;
+    for (int q = 0; q < WAVES; ++q) run += q < wv ? sh.part[q] : 0;
+    if (run < want && (run + sum >= want || tid == USED - 1) && tid < USED) {
         int at = PER - 1;
         bool found = false;
 #pragma unroll
@@ -140,10 +143,8 @@ __device__ __forceinline__ uint32_t find_bin(Shared<WAVES> &sh, uint64_t want, u
             }
             run += found ? 0 : v[j];
         }
-        if (lane == src) {
-            sh.bin = (uint32_t)(lane * PER + at);
-            sh.above = run;
-        }
+        sh.bin = (uint32_t)(tid * PER + at);
+        sh.above = run;
     }
     __syncthreads();
     *above = sh.above;
@@ -169,6 +170,37 @@ __device__ __forceinline__ uint32_t few(Shared<WAVES> &sh, uint32_t n, uint32_t 
             equal += kj == k ? vj : 0;
         }
         if (k && above < want && want <= above + equal) {  // (equal keys write the same)
+            sh.bin = k;
+            sh.above = above;
+        }
+    }
+    __syncthreads();
+    *above_edge = sh.above;
+    return sh.bin;
+}
+
+// As few() for n up to a thread a key, the values in the histogram's room.
+template <int WAVES, class Value>
+__device__ __forceinline__ uint32_t some(Shared<WAVES> &sh, uint32_t n, uint32_t from, uint64_t want, Value value,
+                                         uint64_t *above_edge) {
+    static_assert(WAVES * 64 <= BINS && WAVES * 64 <= LIST, "a place a thread");
+    const uint32_t x = threadIdx.x < n ? sh.list[threadIdx.x] : 0, k = x >= from ? x : 0;
+    __syncthreads();
+    sh.list[threadIdx.x] = k;
+    sh.hist[threadIdx.x] = k ? value(k) : 0;
+    __syncthreads();
+    if (k) {
+        uint64_t above = 0, equal = 0;
+        for (uint32_t j = 0; j < n; j += 8) {  // (behind n: keys 0)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t kj = sh.list[j + i];
+                const uint64_t vj = sh.hist[j + i];
+                above += kj > k ? vj : 0;
+                equal += kj == k ? vj : 0;
+            }
+        }
+        if (above < want && want <= above + equal) {  // (equal keys write the same)
             sh.bin = k;
             sh.above = above;
         }
@@ -727,8 +759,8 @@ __device__ __forceinline__ Edge edge_of_count(Shared<LONG_WAVES> &sh, const Samp
     Edge e;
     uint64_t above;
     if ((uint64_t)a.top_k < total) {
-        const uint32_t k = n <= 64 ? few<WAVES>(sh, n, e.edge, (uint64_t)a.top_k, one, &above)
-                                   : descend<WAVES>(sh, (uint64_t)a.top_k, [&](auto f) { each(e, f, one); }, &above);
+        const uint32_t k = n <= WAVES * 64 ? some<WAVES>(sh, n, e.edge, (uint64_t)a.top_k, one, &above)
+                                           : descend<WAVES>(sh, (uint64_t)a.top_k, [&](auto f) { each(e, f, one); }, &above);
         e.equal = (uint64_t)a.top_k - above;
         e.edge = k;
     }
@@ -741,8 +773,8 @@ __device__ __forceinline__ Edge edge_of_count(Shared<LONG_WAVES> &sh, const Samp
         if (e.equal != ~0ull) sum += e.equal * weigh(e.edge);
         const uint64_t want = share(a.top_p, sum);
         // (the edge takes part with all its equals: one that step 1 cut has its own limit)
-        const uint32_t k = n <= 64 ? few<WAVES>(sh, n, e.edge, want, weigh, &above)
-                                   : descend<WAVES>(sh, want, [&](auto f) { each(e, f, weigh); }, &above);
+        const uint32_t k = n <= WAVES * 64 ? some<WAVES>(sh, n, e.edge, want, weigh, &above)
+                                           : descend<WAVES>(sh, want, [&](auto f) { each(e, f, weigh); }, &above);
         e.by_weight(k, want, above, weigh(k));
     }
     return e;
@@ -796,8 +828,8 @@ __global__ __launch_bounds__(LONG_THREADS) void k_sample_sums(const E *__restric
         if (FORM == 1) {
             // (the list is the boundary's bin alone; the row stands for all bins)
             const uint64_t rest = listed ? want - over : want;
-            const uint32_t k = n <= 64 ? few<WAVES>(sh, n, e.edge, rest, weigh, &above)
-                                       : descend<WAVES>(sh, rest, [&](auto f) { each(e, f, weigh); }, &above);
+            const uint32_t k = n <= WAVES * 64 ? some<WAVES>(sh, n, e.edge, rest, weigh, &above)
+                                               : descend<WAVES>(sh, rest, [&](auto f) { each(e, f, weigh); }, &above);
             e.by_weight(k, rest, above, weigh(k));
         } else {
             e = edge_of_count(sh, a, weigh, n, st.n, each);
@@ -889,11 +921,14 @@ __global__ __launch_bounds__(LONG_THREADS) void k_sample_few(const E *__restrict
                                                              const float *__restrict__ u, SampleArgs a, Work w,
                                                              int32_t *__restrict__ winners,
                                                              int32_t *__restrict__ n_win) {
-    constexpr int WAVES = LONG_WAVES, SLOTS = LIST / LONG_THREADS;
+    constexpr int WAVES = LONG_WAVES;
     __shared__ Shared<WAVES> sh;
-    __shared__ uint64_t ent[LIST], wt[LIST];
+    __shared__ uint64_t ent[LIST], wt[LIST], lead[LIST];  // entries, their weights, the weight before them
     const int64_t b = blockIdx.x;
     const int tid = threadIdx.x;
+    const uint32_t n = w.count[b];
+    const uint64_t mine = w.list[b * LIST + tid];  // (any bits behind n)
+    const float draw = u[b];
     const RowStat st(w.part + b * w.splits, w.splits, a.temperature);
     if (st.n == 0) {  // nothing can win (uniform)
         if (tid < 4) winners[b * 4 + tid] = -1;
@@ -901,55 +936,52 @@ __global__ __launch_bounds__(LONG_THREADS) void k_sample_few(const E *__restrict
         return;
     }
     const Weigher weigh = weigher<WAVES>(sh, a, key_of(st.top));
-    const uint32_t n = w.count[b];
     const uint64_t min_w = (uint64_t)ceil(ldexp((double)a.min_p, a.shift));
     const uint8_t *tf = t_first ? t_first + b * a.N : nullptr;
     __syncthreads();
     if (n <= LIST) {
-        for (uint32_t i = tid; i < n; i += LONG_THREADS) {
-            ent[i] = w.list[b * LIST + i];
-            wt[i] = weigh((uint32_t)(ent[i] >> 32));
+        const uint32_t n8 = (n + 7) / 8 * 8;  // (entries 0 up to here: behind all others, of no weight)
+        for (uint32_t i = tid; i < n8; i += LONG_THREADS) {
+            const uint64_t x = i >= n ? 0 : i < LONG_THREADS ? mine : w.list[b * LIST + i];
+            ent[i] = x;
+            wt[i] = i < n ? weigh((uint32_t)(x >> 32)) : 0;
         }
         __syncthreads();
-        uint64_t before[SLOTS], sum = 0;
-        bool in[SLOTS];
-#pragma unroll
-        for (int q = 0; q < SLOTS; ++q) {
-            const uint32_t i = tid + q * LONG_THREADS;
-            before[q] = 0;
-            in[q] = false;
-            if (i >= n) continue;
+        uint64_t sum = 0;
+        for (uint32_t i = tid; i < n; i += LONG_THREADS) {
             const uint64_t x = ent[i];
+            uint64_t before = 0;
             uint32_t rank = 0;
-            for (uint32_t j = 0; j < n; ++j) {
-                const bool first = ent[j] > x;
-                rank += first;
-                before[q] += first ? wt[j] : 0;
+            for (uint32_t j = 0; j < n8; j += 8) {
+#pragma unroll
+                for (int o = 0; o < 8; ++o) {
+                    const bool first = ent[j + o] > x;
+                    rank += first;
+                    before += first ? wt[j + o] : 0;
+                }
             }
-            in[q] = rank < (uint32_t)a.top_k;
-            sum += in[q] ? wt[i] : 0;
+            const bool in = rank < (uint32_t)a.top_k;
+            lead[i] = in ? before : ~0ull;
+            sum += in ? wt[i] : 0;
         }
-        sum = block_sum<WAVES>(sh, sum);
+        sum = block_sum<WAVES>(sh, sum);  // (after its barriers the weights have been read)
         const uint64_t want = a.top_p < 1.0f ? share(a.top_p, sum) : ~0ull;
         sum = 0;
-        uint64_t own[SLOTS];
-#pragma unroll
-        for (int q = 0; q < SLOTS; ++q) {
-            const uint32_t i = tid + q * LONG_THREADS;
-            own[q] = 0;
-            if (i >= n) continue;
-            if (in[q] && before[q] < want && wt[i] >= min_w) own[q] = wt[i];
-            wt[i] = own[q];  // (the weights of all were read before the sum's barriers)
-            sum += own[q];
+        for (uint32_t i = tid; i < n; i += LONG_THREADS) {
+            const uint64_t own = lead[i] < want && wt[i] >= min_w ? wt[i] : 0;
+            wt[i] = own;
+            sum += own;
         }
-        const uint64_t target = target_of(u[b], block_sum<WAVES>(sh, sum));
-#pragma unroll
-        for (int q = 0; q < SLOTS; ++q) {
-            if (own[q] == 0) continue;
-            const uint32_t i = tid + q * LONG_THREADS, x = (uint32_t)ent[i];
+        const uint64_t target = target_of(draw, block_sum<WAVES>(sh, sum));
+        for (uint32_t i = tid; i < n; i += LONG_THREADS) {
+            if (wt[i] == 0) continue;
+            const uint32_t x = (uint32_t)ent[i];
             uint64_t run = 0;
-            for (uint32_t j = 0; j < n; ++j) run += (uint32_t)ent[j] > x ? wt[j] : 0;  // (a lower index)
-            if (target >= run && target < run + own[q]) {
+            for (uint32_t j = 0; j < n8; j += 8) {
+#pragma unroll
+                for (int o = 0; o < 8; ++o) run += (uint32_t)ent[j + o] > x ? wt[j + o] : 0;  // (a lower index)
+            }
+            if (target >= run && target < run + wt[i]) {
                 const int64_t at = (uint32_t)~x;
                 put_winner(winners, n_win, b, at, tf ? (int)tf[at] : 0, a);
             }
@@ -969,7 +1001,7 @@ __global__ __launch_bounds__(LONG_THREADS) void k_sample_few(const E *__restrict
     });
     sum = block_sum<WAVES>(sh, sum);
     eqs = block_sum<WAVES>(sh, eqs);
-    const uint64_t target = target_of(u[b], sum + (eqs < e.equal ? eqs : e.equal) * we);
+    const uint64_t target = target_of(draw, sum + (eqs < e.equal ? eqs : e.equal) * we);
     const int64_t per = (a.N + LONG_THREADS - 1) / LONG_THREADS, i0 = min(a.N, tid * per), i1 = min(a.N, i0 + per);
     int64_t at;
     if (pick<WAVES>(sh, weigh, we, e, min_w, target, 0, 0, i1 - i0, [&](int64_t i) {
