@@ -10,9 +10,12 @@
 //
 // Rows of up to 16 keys a thread stay in registers.  Longer ones go through
 // launches of several workgroups a row (largest score; histogram; the keys of the
-// boundary's bin; sums by index; the draw), each reading the row again: a step is
-// bound by reading the row, and where it weighs scores by some 30 instructions for
-// each, half of them in double precision.
+// boundary's bin; sums by index; the draw), each reading the row again; where top_k
+// keeps few, the list holds all that matters and the last two are one launch of
+// a workgroup a row.  256 rows of 200003 floats: 33 us to read for the largest (6.2
+// TB/s, half of it from the cache behind HBM), 61 for the histogram of weights (some
+// 36 instructions a score), 39 for the list, 55 for the sums, 14 for the draw.  A row of 131072
+// bfloat16 scores, top_k 50: 4 + 5 + 8 + 10 us, the latency of four dependent steps.
 #include <algorithm>
 #include <cmath>
 
@@ -89,15 +92,18 @@ struct Weigher {
     }
 };
 
+constexpr int SHORT_BINS = 512;  // of a short row
+constexpr int LONG_WAVES = 16, LONG_THREADS = LONG_WAVES * 64;
+
 // LDS of a row's workgroup of WAVES waves.
 template <int WAVES>
 struct Shared {
-    uint64_t hist[BINS];
+    uint64_t hist[WAVES == LONG_WAVES ? BINS : SHORT_BINS];
     double pow[POW];
     uint64_t part[WAVES], part2[WAVES];
     uint64_t above;
     uint32_t bin, n_list;
-    uint32_t list[LIST];
+    uint32_t list[WAVES == LONG_WAVES ? LIST : 64];
 };
 
 // Sum over the workgroup, in every thread.
@@ -183,7 +189,7 @@ __device__ __forceinline__ uint32_t few(Shared<WAVES> &sh, uint32_t n, uint32_t 
 template <int WAVES, class Value>
 __device__ __forceinline__ uint32_t some(Shared<WAVES> &sh, uint32_t n, uint32_t from, uint64_t want, Value value,
                                          uint64_t *above_edge) {
-    static_assert(WAVES * 64 <= BINS && WAVES * 64 <= LIST, "a place a thread");
+    static_assert(WAVES == LONG_WAVES && LONG_THREADS <= BINS && LONG_THREADS <= LIST, "a place a thread");
     const uint32_t x = threadIdx.x < n ? sh.list[threadIdx.x] : 0, k = x >= from ? x : 0;
     __syncthreads();
     sh.list[threadIdx.x] = k;
@@ -269,7 +275,7 @@ __device__ __forceinline__ void put_winner(int32_t *winners, int32_t *n_win, int
 
 template <int WAVES>
 __device__ __forceinline__ Weigher weigher(Shared<WAVES> &sh, const SampleArgs &a, uint32_t ktop) {
-    if (threadIdx.x < POW) sh.pow[threadIdx.x] = exp2(threadIdx.x * (1.0 / POW));
+    for (int i = threadIdx.x; i < POW; i += WAVES * 64) sh.pow[i] = exp2(i * (1.0 / POW));
     Weigher w;
     w.top = (double)value_of(ktop);
     w.per = a.temperature > 0.0f ? 1.4426950408889634074 / (double)a.temperature : 0.0;
@@ -361,8 +367,6 @@ struct Bins {
     }
 };
 
-constexpr int SHORT_BINS = 512;  // of a short row
-
 // As descend(), by a histogram of SHORT_BINS bins first and then the boundary's
 // bin alone, whose keys are few as a rule.
 template <int WAVES, class Each, class Value>
@@ -396,7 +400,9 @@ __device__ __forceinline__ uint32_t boundary(Shared<WAVES> &sh, const Bins &bins
 }
 
 // Grid: one workgroup per image, whose row of at most 16 keys a thread stays in
-// registers; a thread's keys follow each other in index.
+// registers; a thread's keys follow each other in index.  Read once; bound by the
+// chain of short steps between barriers (1000 masked images of 200x4x4 in 21 us,
+// 0.8 TB/s; a single image 10).
 template <class E, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 4) void k_sample_short(const E *__restrict__ scores,
                                                              const uint8_t *__restrict__ t_first,
@@ -514,7 +520,6 @@ __global__ __launch_bounds__(WAVES * 64, 4) void k_sample_short(const E *__restr
     put_winner(winners, n_win, b, i0 + at, tf ? (int)tf[i0 + at] : 0, a);
 }
 
-constexpr int LONG_WAVES = 16, LONG_THREADS = LONG_WAVES * 64;
 constexpr int SPLITS = 64;  // workgroups of a row at most
 
 // Calls f(score, index) for the indices i0 <= index < i1 of a row, by `threads`
@@ -1013,10 +1018,13 @@ __global__ __launch_bounds__(LONG_THREADS) void k_sample_few(const E *__restrict
 
 constexpr int64_t SHORT_MAX = 16 * 64 * 16;  // keys of a row that the registers of a workgroup take
 
-// Workgroups of a long row: about two for each of 256 CUs in all, no less than
-// 4096 scores each.
+// Workgroups of a long row: one for each of 256 CUs in all (two of 1024 threads do
+// not fit a CU's registers together: 32 rows of 131072 take 67 us with twice as
+// many, 53 with these, 62 with half), and no less than 4096 scores each (8 rows of
+// 50001 bfloat16 scores, top_k 50: 30.0 us from 2048 scores on, 28.6 from 4096; a row
+// of 17000: 36.7 from 4096, 39.3 from 8192).
 int splits_of(int B, int64_t N) {
-    int64_t s = 512 / B;
+    int64_t s = 256 / B;
     s = s < N / 4096 ? s : N / 4096;
     return (int)(s < 1 ? 1 : s > SPLITS ? SPLITS : s);
 }
@@ -1038,14 +1046,21 @@ void launch(const void *scores, const uint8_t *t_first, const float *u, int B, c
             int32_t *n_winners, void *ws, hipStream_t st) {
     const E *x = static_cast<const E *>(scores);
     const dim3 rows((unsigned)B), threads(LONG_THREADS);
-    if (a.N <= 4 * 64 * 16) {
-        hipLaunchKernelGGL((k_sample_short<E, 4>), rows, dim3(256), 0, st, x, t_first, u, a, winners, n_winners);
-        return;
+    // As few waves as hold the row, so that more workgroups share a CU and one's steps
+    // fill the other's waits: 1000 rows of 2000 take 17.7 us with two waves each, 21.7
+    // with four; of 8000 45 us with eight, 95 with sixteen, 121 by the launches below
+    // (of 16000: 120 with sixteen, 148 below; 16 such rows 37.3 and 38.6).
+#define SPK_SHORT(WAVES)                                                                                        \
+    if (a.N <= WAVES * 64 * 16) {                                                                               \
+        hipLaunchKernelGGL((k_sample_short<E, WAVES>), rows, dim3(WAVES * 64), 0, st, x, t_first, u, a, winners, \
+                           n_winners);                                                                          \
+        return;                                                                                                 \
     }
-    if (a.N <= SHORT_MAX) {
-        hipLaunchKernelGGL((k_sample_short<E, 16>), rows, threads, 0, st, x, t_first, u, a, winners, n_winners);
-        return;
-    }
+    SPK_SHORT(2)
+    SPK_SHORT(4)
+    SPK_SHORT(8)
+    SPK_SHORT(16)
+#undef SPK_SHORT
     Work w;
     carve(ws, B, a.N, &w);
     const dim3 grid((unsigned)w.splits, (unsigned)B);
