@@ -198,10 +198,10 @@ __device__ __forceinline__ void to_lds(char *dst, const char *src, int n, int wa
                      "{m0}"(__builtin_amdgcn_readfirstlane((int)(at + o)))
                      : "memory");
 }
-// All of the wave's copies and loads have arrived, its stores are out.  (As a
-// builtin the compiler counts it too: loads before it need no wait of their own.)
 // A barrier that hands LDS over; copies and loads may stay in flight.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// All of the wave's copies and loads have arrived, its stores are out.  (As a
+// builtin the compiler counts it too: loads before it need no wait of their own.)
 __device__ __forceinline__ void wait_copies() {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)

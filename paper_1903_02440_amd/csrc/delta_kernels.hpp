@@ -102,7 +102,8 @@ struct PrepLds {
 //     T_ij = -T_ii sum over j <= m < i of A_im T_mj
 // on the float matrix cores, a block column a wave.  The steps are short and
 // wait for each other, so the LDS is kept small enough for four workgroups a CU
-// (dk <= 128, bfloat16).
+// (dk <= 128, bfloat16).  4 x 4096 samples of 16 keys for 32 heads of 128x128,
+// bfloat16: 150 us, 1.5 TB/s written and read, 190 with the products in LDS.
 template <class E, int DS, bool BWD>
 __global__ __launch_bounds__(PREP_THREADS, 4) void k_delta_prep(const E *__restrict__ q, const E *__restrict__ k,
                                                                 const float *__restrict__ g,
@@ -304,7 +305,10 @@ __device__ __forceinline__ int head_of(int x, int n) { return n % 8 == 0 ? (x & 
 // Waves of a workgroup that only copy the next chunk's operands to LDS.  The
 // copies go out at some 64 bytes a cycle and CU, and a wave that issues them
 // waits for that (2400 of 7100 cycles of a chunk of 250x10 memories, float, and
-// as much of 11000 of 128x128 ones, bfloat16).
+// as much of 11000 of 128x128 ones, bfloat16).  1024 samples of 16 memories of
+// 128x128, float: 79 us with two such waves, 73 with four; 4 x 4096 samples of 32,
+// bfloat16: 425 us with two, 435 with four, 615 with eight, whose registers the
+// other waves lack.
 constexpr int COPIERS = 4;
 
 // Waves that carry columns, at most: those of one kernel are limited by their
@@ -314,11 +318,12 @@ constexpr int carriers() {
     return DS == 8 && KS == 1 ? 4 : 8;
 }
 
-// LDS of the states' kernel, for KS waves to a tile of 16 columns.  K is needed all through a chunk and has two buffers where they
-// fit; T, the coefficients and P from the middle on, with two where those still
-// fit; Q is done with in the middle and has one, or none (DIRECT) where K's second
-// only fits without it and a wave has registers for its own part of Q.  Then the
-// partial sums that the waves of a tile exchange.
+// LDS of the states' kernel, for KS waves to a tile of 16 columns.  K is needed all
+// through a chunk and has two buffers where they fit; T, the coefficients and P from
+// the middle on, with two where those still fit; Q is done with in the middle and
+// has one, or none (DIRECT) where K's second only fits without it and a wave has
+// registers for its own part of Q.  Then the partial sums that the waves of a tile
+// exchange.
 template <class E, int DS, int KS, bool STATES>
 struct ScanLds {
     using F = Blob<E, DS, STATES>;
@@ -340,8 +345,12 @@ struct ScanLds {
 // registers: as the right operand of K S and Q S (three terms) and as the sums of
 // K^T (last U).  They add up K S through LDS in the middle of a chunk, after
 // which each has U for itself; of out each finishes some rows.  KS = 1 where the
-// columns alone fill the SIMDs, more where they do not.  STATES: for the backward pass, the state that enters each chunk
-// and U are written instead of out (`kept`).
+// columns alone fill the SIMDs, more where they do not.  STATES: for the backward
+// pass, the state that enters each chunk and U are written instead of out (`kept`).
+// The chunks of a head follow each other: bound by a chunk's chain of products,
+// splits and two exchanges, 2.6 us for 32 samples of 250x10 memories, float (1000
+// samples 84 us), 5.0 us for 64 of 128x128, bfloat16 (4 x 4096 samples of 32 heads
+// 320 us, 160 TFLOP/s of the definition's products).
 template <class E, int DS, int KS, bool STATES>
 __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_scan(const E *__restrict__ v, Args a,
                                                     const int32_t *__restrict__ lengths, int tiles, Chunks w,
@@ -596,18 +605,27 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
 }
 
 // How a call's columns go to waves: KS waves to a tile of 16 columns and `tiles`
-// of them a workgroup (`threads` in all), out of `all` tiles a head.
+// of them a workgroup (`threads` in all), out of `all` tiles a head.  A CU's LDS
+// takes one workgroup, so more than 256 would wait for a second turn (8 ragged
+// sequences of 1531, 8 memories of 96x72, bfloat16: 114 us in 192 workgroups, 166 in 320).
+// Up to there a tile's sums over dk are shared by up to eight waves, while the
+// 1024 SIMDs have no more than one wave each (1000 samples of 8 memories of 250x10,
+// float: 103 us with eight, 175 with one; 2 x 1024 of 16 of 256x256, bfloat16: 117
+// with one, 108 with two, 117 with four), and tiles spread over more workgroups
+// (2048 samples of 8 memories of 128x64, bfloat16: 135 us with two tiles each, 112
+// with one).
 struct Cols {
     int KS, tiles, blocks, threads;
 };
 inline Cols columns(const Args &a, int all, int DS) {
     Cols c;
-    const int64_t waves = (int64_t)a.B * a.Hv * all;
+    const int64_t heads = (int64_t)a.B * a.Hv;
+    auto groups = [&](int tiles) { return heads * ((all + tiles - 1) / tiles); };
     c.KS = 1;
-    while (c.KS < 8 && 2 * c.KS <= DS && waves * c.KS <= 1024) c.KS *= 2;  // up to two waves on each of 1024 SIMDs
+    while (c.KS < 8 && 2 * c.KS <= DS && heads * all * 2 * c.KS <= 1024 && groups(8 / (2 * c.KS)) <= 256) c.KS *= 2;
     const int most = (DS == 8 && c.KS == 1 ? 4 : 8) / c.KS;
     c.tiles = all < most ? all : most;
-    while (c.tiles > 1 && (int64_t)a.B * a.Hv * ((all + c.tiles - 1) / c.tiles) < 256) c.tiles = (c.tiles + 1) / 2;
+    while (c.tiles > 1 && groups((c.tiles + 1) / 2) <= 256) c.tiles = (c.tiles + 1) / 2;
     c.blocks = (all + c.tiles - 1) / c.tiles;
     c.threads = 64 * (c.tiles * c.KS + COPIERS);
     return c;
