@@ -49,7 +49,9 @@ enum { SPK_F32 = 0, SPK_BF16 = 1 };
  *              initial_state (updated in place).  A sequence of no samples
  *              leaves its state as it was.
  * All sums and states are held in float; bfloat16 inputs are exact terms of
- * the products.  Repeated calls give the same bits.
+ * the products.  Repeated calls give the same bits.  Inputs up to the lengths
+ * are to be finite (g may be -inf): one that is not makes outputs of its own
+ * sequence and head non-finite, up to 63 samples before it too.
  * Limits: 1 <= dk <= 256, 1 <= dv <= 4096, Hv a multiple of Hk, B*Hv <= 65535,
  * Hv*dv <= 2^22, L <= 2^24.  Workspace: spk_delta_rule_workspace_size(...) bytes.          */
 SPK_API size_t spk_delta_rule_workspace_size(int dtype, int B, int L, int Hk, int Hv, int dk, int dv);
