@@ -79,8 +79,9 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
     };
     const int64_t vstep = (int64_t)a.Hv * a.dv;
     const E *orow = d_out + ((int64_t)b * a.L * a.Hv + h) * a.dv;
-    const uint32_t lin = (uint32_t)((4 * gr * vstep + min(col, a.dv - 1)) * sizeof(E)),
-                   lkept = (uint32_t)(4 * gr * kept.dvp + col) * 4, lstate = (uint32_t)(8 * gr * kept.dvp + col) * 4;
+    const uint32_t lin = (uint32_t)((4 * gr * vstep + min(col, a.dv - 1)) * sizeof(E));
+    const int ct = (int)blockIdx.y * tiles + tile, vgs = kept.dvp / 32;
+    const uint32_t lkept = block_place(ct, lane);
     E on[MT][4];
     auto upstream = [&](int c) {
         const E *p = orow + (int64_t)c * C * vstep;
@@ -110,12 +111,9 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
         const float *co = reinterpret_cast<const float *>(H);
         f32x4 X[MT], Y[MT];
         if (mine) {
-            float *dst = kept.dS + ((int64_t)bh * w.NC + c) * 32 * DS * kept.dvp;
+            f32x4 *dst = kept.dS + ((((int64_t)bh * w.NC + c) * 2 * DS + 2 * s0) * vgs + (ct >> 1)) * KEPT_BLOCK;
 #pragma unroll
-            for (int t = 0; t < 2 * DW; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    at(dst + (32 * (s0 + (t >> 1)) + 4 * (t & 1) + r) * kept.dvp, lstate) = S[t][r];
+            for (int t = 0; t < 2 * DW; ++t) at(dst + t * vgs * KEPT_BLOCK, lkept) = quad_transpose(S[t], lane);
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) X[mt] = Y[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -208,13 +206,10 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
         }
         if (c > 0) fetch_rest(c - 1);
         if (mine) {
-            float *yd = kept.Y + ((int64_t)bh * w.NC + c) * C * kept.dvp;
+            f32x4 *yd = kept.Y + (((int64_t)bh * w.NC + c) * MT * vgs + (ct >> 1)) * KEPT_BLOCK;
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                if (part != mt * KS / MT) continue;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) at(yd + (16 * mt + r) * kept.dvp, lkept) = Y[mt][r];
-            }
+            for (int mt = 0; mt < MT; ++mt)
+                if (part == mt * KS / MT) at(yd + mt * vgs * KEPT_BLOCK, lkept) = quad_transpose(Y[mt], lane);
         }
     }
     if (!live || !d_first) return;
@@ -227,9 +222,60 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
         }
 }
 
-template <class E>
-struct alignas(4 * sizeof(E)) Four {
-    E e[4];
+// Eight neighbouring elements of a row as they were loaded: taken apart only where
+// they are used, since taking them apart waits for them.  WIDE: rows of dv elements
+// go four at a time.
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+template <class E, bool WIDE>
+struct Eight {
+    E e[8];
+    __device__ __forceinline__ void load(const E *row, int c, int dv) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = row[min(c + j, dv - 1)];
+    }
+    __device__ __forceinline__ float get(int j) const { return to_float(e[j]); }
+    static __device__ __forceinline__ void store(E *row, int c, int dv, const float (&x)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (c + j < dv) row[c + j] = from_float<E>(x[j]);
+    }
+};
+template <>
+struct Eight<float, true> {
+    f32x4 e[2];
+    __device__ __forceinline__ void load(const float *row, int c, int dv) {
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) e[hf] = *reinterpret_cast<const f32x4 *>(row + min(c + 4 * hf, dv - 4));
+    }
+    __device__ __forceinline__ float get(int j) const { return e[j >> 2][j & 3]; }
+    static __device__ __forceinline__ void store(float *row, int c, int dv, const float (&x)[8]) {
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf)
+            if (c + 4 * hf < dv)
+                *reinterpret_cast<f32x4 *>(row + c + 4 * hf) = (f32x4){x[4 * hf], x[4 * hf + 1], x[4 * hf + 2], x[4 * hf + 3]};
+    }
+};
+template <>
+struct Eight<uint16_t, true> {
+    u32x2 e[2];
+    __device__ __forceinline__ void load(const uint16_t *row, int c, int dv) {
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) e[hf] = *reinterpret_cast<const u32x2 *>(row + min(c + 4 * hf, dv - 4));
+    }
+    __device__ __forceinline__ float get(int j) const {
+        const uint32_t w = e[j >> 2][(j >> 1) & 1];
+        return __uint_as_float(j & 1 ? w & 0xFFFF0000u : w << 16);
+    }
+    static __device__ __forceinline__ void store(uint16_t *row, int c, int dv, const float (&x)[8]) {
+        auto two = [](float lo, float hi) {
+            return (uint32_t)from_float<uint16_t>(lo) | ((uint32_t)from_float<uint16_t>(hi) << 16);
+        };
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf)
+            if (c + 4 * hf < dv)
+                *reinterpret_cast<u32x2 *>(row + c + 4 * hf) =
+                    (u32x2){two(x[4 * hf], x[4 * hf + 1]), two(x[4 * hf + 2], x[4 * hf + 3])};
+    }
 };
 
 constexpr int GRAD_WAVES = 8, GRAD_THREADS = GRAD_WAVES * 64;
@@ -258,17 +304,17 @@ struct GradLds {
 // terms' products of a float sum with another and their splits, with one workgroup
 // a CU (145 KB of LDS at 128 rows, bfloat16): waits take 59 % of the waves' time.
 // 2 x 2048 samples of 16 keys for 32 heads of 128x128: 310 us, 1.7 TB/s.
-template <class E, int DS>
+template <class E, int DS, bool WIDE>
 __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
     const E *__restrict__ v, const float *__restrict__ g, const E *__restrict__ d_out, Args a,
-    const int32_t *__restrict__ lengths, int wide, Chunks w, Kept kept, E *__restrict__ d_q,
+    const int32_t *__restrict__ lengths, Chunks w, Kept kept, E *__restrict__ d_q,
     E *__restrict__ d_k, E *__restrict__ d_v, float *__restrict__ d_g, float *__restrict__ d_beta) {
     using F = Blob<E, DS, true>;
     using G = GradLds<E, DS>;
     constexpr int C = F::C, MT = F::MT, NT = F::NT, GP = F::GP, PITCH = G::PITCH;
     constexpr int TW = (2 * DS + GRAD_WAVES - 1) / GRAD_WAVES;  // dk tiles of a wave
     constexpr int LT = MT * (MT + 1) / 2, LW = (2 * LT + GRAD_WAVES - 1) / GRAD_WAVES;  // tiles of M and N
-    constexpr int TASKS = (3 * MT + GRAD_WAVES - 1) / GRAD_WAVES;                        // tiles of Y, U and dO
+    static_assert(2 * MT <= GRAD_WAVES, "a wave a tile of Y and of U");
     extern __shared__ char lds[];
     const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, gr = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -319,8 +365,9 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
             if (tid < C) gam[tid] = s;
         }
         for (int i = tid; i < 3 * C; i += GRAD_THREADS) co[i] = cog[i];
-        const float *S = kept.S + ch * 32 * DS * kept.dvp, *dS = kept.dS + ch * 32 * DS * kept.dvp;
-        const float *U = kept.U + ch * C * kept.dvp, *Y = kept.Y + ch * C * kept.dvp;
+        const int vgs = kept.dvp / 32;
+        const f32x4 *S = kept.S + ch * 2 * DS * vgs * KEPT_BLOCK, *dS = kept.dS + ch * 2 * DS * vgs * KEPT_BLOCK;
+        const f32x4 *U = kept.U + ch * MT * vgs * KEPT_BLOCK, *Y = kept.Y + ch * MT * vgs * KEPT_BLOCK;
         f32x4 dq[TW][MT], rr[TW][MT], cc[TW][MT], mn[LW];
 #pragma unroll
         for (int p = 0; p < TW; ++p)
@@ -331,85 +378,54 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
         float dot = 0.0f;   // <dS, S>, the lane's part
         float yvp = 0.0f;   // y.v of row 16 wv + m, the lane's part (waves below MT)
         // The wave's share of the next 32 columns is on its way while these are used:
-        // Y, U and dO by tile of samples (Y of tile mt: wave mt), v beside Y, and the
-        // rows of S and dS that are its right operands.
-        f32x4 sn[TW][2], en[TW][2], yu[TASKS][2];
-        Four<E> vo[TASKS][2];
+        // a tile of samples of Y (wave mt) or U (wave MT + mt), with v beside Y and dO
+        // beside U, and the rows of S and dS that are its right operands.  No load
+        // depends on a branch: it would be waited for where the branches meet.
+        const bool of_u = wv >= MT, stages = wv < 2 * MT;
+        const int mt0 = wv % MT, i0 = 16 * mt0 + m;
+        const f32x4 *yu_from = (of_u ? U : Y) + mt0 * vgs * KEPT_BLOCK + lane;
+        const E *vo_from = (of_u ? d_out : v) + ((row0 + min(i0, n - 1)) * a.Hv + h) * a.dv;
+        f32x4 sn[TW][2], en[TW][2], yu[2];
+        Eight<E, WIDE> vo;
         auto load_states = [&](int vg) {
 #pragma unroll
             for (int p = 0; p < TW; ++p) {
                 const int t = min(p * GRAD_WAVES + wv, 2 * DS - 1);
-                const float *ps = S + (int64_t)dk_of(t, m) * kept.dvp + 32 * vg + 4 * gr;
-                const float *pd = dS + (int64_t)dk_of(t, m) * kept.dvp + 32 * vg + 4 * gr;
+                const int at = (t * vgs + vg) * KEPT_BLOCK + lane;
 #pragma unroll
                 for (int hf = 0; hf < 2; ++hf) {
-                    sn[p][hf] = *reinterpret_cast<const f32x4 *>(ps + 16 * hf);
-                    en[p][hf] = *reinterpret_cast<const f32x4 *>(pd + 16 * hf);
+                    sn[p][hf] = S[at + 64 * hf];
+                    en[p][hf] = dS[at + 64 * hf];
                 }
             }
         };
         auto load = [&](int vg) {
             if (TW == 1) load_states(vg);  // (two tiles a wave have no registers to spare for it)
-#pragma unroll
-            for (int x = 0; x < TASKS; ++x) {
-                const int task = min(wv + x * GRAD_WAVES, 3 * MT - 1), which = task / MT, i = 16 * (task % MT) + m;
-                const float *pf = (which == 1 ? U : Y) + (int64_t)i * kept.dvp + 32 * vg + 4 * gr;
-                const E *pe = (which == 2 ? d_out : v) + ((row0 + min(i, n - 1)) * a.Hv + h) * a.dv;
-                if (which < 2) {
-                    yu[x][0] = *reinterpret_cast<const f32x4 *>(pf);
-                    yu[x][1] = *reinterpret_cast<const f32x4 *>(pf + 16);
-                }
-                if (which != 1) {
-                    if (wide) {
-#pragma unroll
-                        for (int hf = 0; hf < 2; ++hf)
-                            vo[x][hf] = *reinterpret_cast<const Four<E> *>(pe + min(32 * vg + 16 * hf + 4 * gr, a.dv - 4));
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) vo[x][j >> 2].e[j & 3] = pe[min(32 * vg + slot(gr, j), a.dv - 1)];
-                    }
-                }
-            }
+            yu[0] = yu_from[vg * KEPT_BLOCK];
+            yu[1] = yu_from[vg * KEPT_BLOCK + 64];
+            vo.load(vo_from, 32 * vg + 8 * gr, a.dv);
         };
         load(0);
         for (int vg = 0; vg < kept.dvp / 32; ++vg) {
             __syncthreads();  // the staged columns (and, at first, the coefficients) may be written
+            if (stages) {
+                const int cv = 32 * vg + 8 * gr;
+                const float y[8] = {yu[0][0], yu[0][1], yu[0][2], yu[0][3], yu[1][0], yu[1][1], yu[1][2], yu[1][3]};
+                float x[8];
 #pragma unroll
-            for (int x = 0; x < TASKS; ++x) {
-                const int task = wv + x * GRAD_WAVES, which = task / MT, mt = task % MT, i = 16 * mt + m;
-                if (task >= 3 * MT) continue;
-                float y[8];
-                if (which < 2) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) y[j] = yu[x][j >> 2][j & 3];
-                    put_frag<3>((which ? fu : fy) + mt * 3 * FRAG, lane, split<3>(y));
-                    if (which == 0) {
-                        const int64_t vrow = ((row0 + min(i, n - 1)) * a.Hv + h) * a.dv;
-                        const float be = co[C + i];
-                        Four<E> dv4[2];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const bool in = i < n && 32 * vg + slot(gr, j) < a.dv;
-                            yvp += in ? y[j] * to_float(vo[x][j >> 2].e[j & 3]) : 0.0f;
-                            dv4[j >> 2].e[j & 3] = from_float<E>(be * y[j]);
-                        }
-#pragma unroll
-                        for (int hf = 0; hf < 2; ++hf) {
-                            const int cv = 32 * vg + 16 * hf + 4 * gr;
-                            if (wide) {
-                                if (i < n && cv < a.dv) *reinterpret_cast<Four<E> *>(d_v + vrow + cv) = dv4[hf];
-                            } else {
-#pragma unroll
-                                for (int j = 0; j < 4; ++j)
-                                    if (i < n && cv + j < a.dv) d_v[vrow + cv + j] = dv4[hf].e[j];
-                            }
-                        }
-                    }
+                for (int j = 0; j < 8; ++j) x[j] = i0 < n && cv + j < a.dv ? vo.get(j) : 0.0f;
+                put_frag<3>((of_u ? fu : fy) + mt0 * 3 * FRAG, lane, split<3>(y));
+                if (of_u) {
+                    put_frag<NT>(fo + mt0 * NT * FRAG, lane, split<NT>(x));
                 } else {
+                    const float be = co[C + i0];
+                    float d[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        y[j] = i < n && 32 * vg + slot(gr, j) < a.dv ? to_float(vo[x][j >> 2].e[j & 3]) : 0.0f;
-                    put_frag<NT>(fo + mt * NT * FRAG, lane, split<NT>(y));
+                    for (int j = 0; j < 8; ++j) {
+                        yvp += cv + j < a.dv && i0 < n ? y[j] * x[j] : 0.0f;
+                        d[j] = be * y[j];
+                    }
+                    if (i0 < n) Eight<E, WIDE>::store(d_v + ((row0 + i0) * a.Hv + h) * a.dv, cv, a.dv, d);
                 }
             }
             if (TW > 1) load_states(vg);
@@ -619,10 +635,10 @@ size_t carve(void *ws, const Args &a, Chunks *w, Kept *kept) {
     kept->dvp = (a.dv + 31) / 32 * 32;
     w->key = c.take<char>((size_t)a.B * a.Hk * w->NC * F::KEY);
     w->head = c.take<char>(bh * w->NC * F::HEAD);
-    kept->S = c.take<float>(bh * w->NC * 32 * DS * kept->dvp);
-    kept->dS = c.take<float>(bh * w->NC * 32 * DS * kept->dvp);
-    kept->U = c.take<float>(bh * w->NC * F::C * kept->dvp);
-    kept->Y = c.take<float>(bh * w->NC * F::C * kept->dvp);
+    kept->S = c.take<f32x4>(bh * w->NC * 8 * DS * kept->dvp);
+    kept->dS = c.take<f32x4>(bh * w->NC * 8 * DS * kept->dvp);
+    kept->U = c.take<f32x4>(bh * w->NC * F::C / 4 * kept->dvp);
+    kept->Y = c.take<f32x4>(bh * w->NC * F::C / 4 * kept->dvp);
     return spk::align_up(c.off, 256);
 }
 
@@ -665,9 +681,12 @@ int backward(const Call &c, const Args &a, void *ws, hipStream_t st, const char 
 #undef SPK_SCAN
     const bool fours = ((reinterpret_cast<uintptr_t>(c.v) | reinterpret_cast<uintptr_t>(c.d_out) |
                          reinterpret_cast<uintptr_t>(c.d_v)) & (4 * sizeof(E) - 1)) == 0;
-    const int wide = a.dv % 4 == 0 && fours;  // rows of dv elements go four at a time
-    hipLaunchKernelGGL((k_delta_grads<E, DS>), per_key, dim3(GRAD_THREADS), LG, st, v, c.g, d_out, a, c.lengths, wide, w,
-                       kept, static_cast<E *>(c.d_q), static_cast<E *>(c.d_k), static_cast<E *>(c.d_v), c.d_g, c.d_beta);
+#define SPK_GRADS(WIDE)                                                                                             \
+    hipLaunchKernelGGL((k_delta_grads<E, DS, WIDE>), per_key, dim3(GRAD_THREADS), LG, st, v, c.g, d_out, a, c.lengths, w, \
+                       kept, static_cast<E *>(c.d_q), static_cast<E *>(c.d_k), static_cast<E *>(c.d_v), c.d_g, c.d_beta)
+    if (a.dv % 4 == 0 && fours) SPK_GRADS(true);
+    else SPK_GRADS(false);
+#undef SPK_GRADS
     return spk::check_launch(name);
 }
 

@@ -29,13 +29,42 @@ struct Chunks {
 };
 
 // What the passes over the chunks keep for the gradients, columns padded to dvp
-// (a multiple of 32) and rows to whole chunks and groups of 32 of dk:
-//   S, dS  f32 [b * Hv + h][chunk][32 DS][dvp]  state that enters the chunk, gradient of the one that leaves it
-//   U, Y   f32 [b * Hv + h][chunk * C][dvp]
+// (a multiple of 32) and rows to whole chunks and groups of 32 of dk, in blocks of
+// 16 rows and 32 columns:
+//   S, dS  [b * Hv + h][chunk][2 DS][dvp / 32]  state that enters the chunk, gradient of the one that leaves it
+//   U, Y   [b * Hv + h][chunk][MT][dvp / 32]
+// A block is in the order in which the gradients' waves take it up as an operand:
+// columns 8g..8g+3 of row i for lane (i, g), then columns 8g+4..8g+7.  (From rows of
+// dvp floats a load gathers 16 rows, a cache line for each 16 bytes.)
+constexpr int KEPT_BLOCK = 128;  // in f32x4
 struct Kept {
     int dvp;
-    float *S, *dS, *U, *Y;
+    f32x4 *S, *dS, *U, *Y;
 };
+
+// Result tile to block: lane (n, g) holds rows 4g..4g+3 of column n, and gets row
+// 4g + n % 4 of the columns 4 (n / 4)... of its quad.
+__device__ __forceinline__ f32x4 quad_transpose(f32x4 a, int lane) {
+    auto swap = [&](float &lo, float &hi, bool up, auto ctrl) {  // hi of the lower lane and lo of the upper one change places
+        const int x = __float_as_int(up ? lo : hi);
+        const float y = __int_as_float(__builtin_amdgcn_update_dpp(x, x, decltype(ctrl)::value, 0xF, 0xF, true));
+        lo = up ? y : lo;
+        hi = up ? hi : y;
+    };
+    float x[4] = {a[0], a[1], a[2], a[3]};
+    const std::integral_constant<int, 0xB1> by1;  // quad lanes 1 0 3 2
+    const std::integral_constant<int, 0x4E> by2;  // quad lanes 2 3 0 1
+    swap(x[0], x[1], lane & 1, by1);
+    swap(x[2], x[3], lane & 1, by1);
+    swap(x[0], x[2], lane & 2, by2);
+    swap(x[1], x[3], lane & 2, by2);
+    return (f32x4){x[0], x[1], x[2], x[3]};
+}
+// the lane's place in a block for a result tile of columns 16 ct.. (bytes)
+__device__ __forceinline__ uint32_t block_place(int ct, int lane) {
+    const int n = lane & 15, g = lane >> 4;
+    return ((n >> 2) & 1) * 1024 + (2 * (ct & 1) + (n >> 3)) * 256 + (4 * g + (n & 3)) * 16;
+}
 
 // Eight elements of a row of keys or queries from 32 s + 8 g on, in the row's own
 // type.  Indices past the row are clamped and the elements set to 0 afterwards:
@@ -395,8 +424,9 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
     const E *vrow = v + ((int64_t)b * a.L * a.Hv + h) * a.dv;
     E *orow = out + ((int64_t)b * a.L * a.Hv + h) * a.dv;
     const uint32_t lin = (uint32_t)((4 * gr * vstep + min(col, a.dv - 1)) * sizeof(E)),
-                   lout = (uint32_t)((4 * gr * vstep + col) * sizeof(E)),
-                   lkept = (uint32_t)(4 * gr * kept.dvp + col) * 4, lstate = (uint32_t)(8 * gr * kept.dvp + col) * 4;
+                   lout = (uint32_t)((4 * gr * vstep + col) * sizeof(E));
+    const int ct = (int)blockIdx.y * tiles + tile, vgs = kept.dvp / 32;
+    const uint32_t lkept = block_place(ct, lane);
     E vv[MT][4];
     auto values = [&](int c) {
         const E *p = vrow + (int64_t)c * C * vstep;
@@ -445,12 +475,9 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
         float vc[MT][4];
         if (mine) {
             if (STATES) {
-                float *dst = kept.S + ((int64_t)bh * w.NC + c) * 32 * DS * kept.dvp;
+                f32x4 *dst = kept.S + ((((int64_t)bh * w.NC + c) * 2 * DS + 2 * s0) * vgs + (ct >> 1)) * KEPT_BLOCK;
 #pragma unroll
-                for (int t = 0; t < 2 * DW; ++t)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        at(dst + (32 * (s0 + (t >> 1)) + 4 * (t & 1) + r) * kept.dvp, lstate) = S[t][r];
+                for (int t = 0; t < 2 * DW; ++t) at(dst + t * vgs * KEPT_BLOCK, lkept) = quad_transpose(S[t], lane);
             }
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) X[mt] = Y[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -565,13 +592,10 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
             if (M::TB == 1) fetch_t(c + 1);
         }
         if (STATES && mine) {
-            float *dst = kept.U + ((int64_t)bh * w.NC + c) * C * kept.dvp;
+            f32x4 *dst = kept.U + (((int64_t)bh * w.NC + c) * MT * vgs + (ct >> 1)) * KEPT_BLOCK;
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                if (part != mt * KS / MT) continue;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) at(dst + (16 * mt + r) * kept.dvp, lkept) = Y[mt][r];
-            }
+            for (int mt = 0; mt < MT; ++mt)
+                if (part == mt * KS / MT) at(dst + mt * vgs * KEPT_BLOCK, lkept) = quad_transpose(Y[mt], lane);
         }
         if (!STATES && live) {
             E *p = orow + (int64_t)c * C * vstep;
