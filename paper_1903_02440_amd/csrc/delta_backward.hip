@@ -355,16 +355,6 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
         const int h = hk * rep + hr;
         const int64_t bh = (int64_t)b * a.Hv + h, ch = bh * w.NC + chunk;
         const float *cog = reinterpret_cast<const float *>(w.head + ch * F::HEAD + F::T);
-        if (tid < 64) {
-            double s = tid < C && tid < n ? log_decay(g[(row0 + tid) * a.Hv + h]) : 0.0;
-#pragma unroll
-            for (int o = 1; o < C; o <<= 1) {
-                const double p = __shfl_up(s, o, 64);
-                if (tid >= o) s += p;
-            }
-            if (tid < C) gam[tid] = s;
-        }
-        for (int i = tid; i < 3 * C; i += GRAD_THREADS) co[i] = cog[i];
         const int vgs = kept.dvp / 32;
         const f32x4 *S = kept.S + ch * 2 * DS * vgs * KEPT_BLOCK, *dS = kept.dS + ch * 2 * DS * vgs * KEPT_BLOCK;
         const f32x4 *U = kept.U + ch * MT * vgs * KEPT_BLOCK, *Y = kept.Y + ch * MT * vgs * KEPT_BLOCK;
@@ -406,6 +396,16 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
             vo.load(vo_from, 32 * vg + 8 * gr, a.dv);
         };
         load(0);
+        if (tid < 64) {
+            double s = tid < C && tid < n ? log_decay(g[(row0 + tid) * a.Hv + h]) : 0.0;
+#pragma unroll
+            for (int o = 1; o < C; o <<= 1) {
+                const double p = __shfl_up(s, o, 64);
+                if (tid >= o) s += p;
+            }
+            if (tid < C) gam[tid] = s;
+        }
+        for (int i = tid; i < 3 * C; i += GRAD_THREADS) co[i] = cog[i];
         for (int vg = 0; vg < kept.dvp / 32; ++vg) {
             __syncthreads();  // the staged columns (and, at first, the coefficients) may be written
             if (stages) {
@@ -567,20 +567,25 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
                 }
             }
         }
+        // Sums over the 16 lanes of a row group: at each step a lane keeps one half of its
+        // values and gives the other away.
+        constexpr int NV = 8 * MT;
+        float x[NV];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int i = 0; i < NV; ++i) x[i] = i & 1 ? pb[i >> 3][(i >> 1) & 3] : pg[i >> 3][(i >> 1) & 3];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
+        for (int s = 8, half = NV / 2; s >= 1; s >>= 1, half >>= 1)
 #pragma unroll
-                for (int s = 8; s >= 1; s >>= 1) {
-                    pg[mt][r] += __shfl_xor(pg[mt][r], s, 64);
-                    pb[mt][r] += __shfl_xor(pb[mt][r], s, 64);
-                }
-                if (m == 0) {
-                    sums[(2 * wv) * C + 16 * mt + 4 * gr + r] = pg[mt][r];
-                    sums[(2 * wv + 1) * C + 16 * mt + 4 * gr + r] = pb[mt][r];
-                }
+            for (int i = 0; i < half; ++i) {
+                const bool up = m & s;
+                const float give = up ? x[i] : x[i + half];
+                x[i] = (up ? x[i + half] : x[i]) + __shfl_xor(give, s, 64);
             }
+#pragma unroll
+        for (int j = 0; j < NV / 16; ++j) {
+            const int i = m * (NV / 16) + j;
+            sums[(2 * wv + (i & 1)) * C + 16 * (i >> 3) + 4 * gr + ((i >> 1) & 3)] = x[j];
+        }
 #pragma unroll
         for (int s = 32; s >= 1; s >>= 1) pe += __shfl_xor(pe, s, 64);
         if (lane == 0) ends[wv] += pe;
