@@ -135,8 +135,10 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+            for (int r = 0; r < 4; ++r) {
                 o[mt][r] = live && c * C + 16 * mt + 4 * gr + r < n ? to_float(on[mt][r]) : 0.0f;
+                made(o[mt][r]);
+            }
         if (c > 0) {
             upstream(c - 1);
             if (M::KB == 2) fetch_k(c - 1);

@@ -96,6 +96,11 @@ __device__ __forceinline__ void as_floats(const Raw8<E> &w, int s, int g, int dk
     for (int j = 0; j < 8; ++j) x[j] = row && 32 * s + 8 * g + j < dk ? to_float(w.e[j]) : 0.0f;
 }
 
+// Has x computed here, before the loads that follow: their registers can then be
+// those of the values that x was made from.  Made later, x would keep these alive,
+// and the new ones would be waited for at once to be moved into their place.
+__device__ __forceinline__ void made(float &x) { asm volatile("" : "+v"(x) : : "memory"); }
+
 constexpr int PREP_THREADS = 256;
 
 // triangular fragment f as (tile of rows, group of summed indices): the lower
@@ -455,6 +460,9 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
                 for (int mt = 0; mt < MT; ++mt) qd[s][mt] = frag<NT>(p + (mt * DS + s0 + s) * NT * FRAG, lane);
         }
     };
+    auto arrived = [&] {  // what the copiers have asked for; the others' loads are waited for where they are used
+        if (cw >= 0) wait_copies();
+    };
     if (nc) {
         if (cw >= 0) {
             fetch_k(0);
@@ -464,7 +472,7 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
             values(0);
             direct_q(0);
         }
-        wait_copies();
+        arrived();
     }
     __syncthreads();
     for (int c = 0; c < nc; ++c) {
@@ -501,6 +509,7 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
                 for (int r = 0; r < 4; ++r) {
                     vc[mt][r] = to_float(vv[mt][r]);
                     if (STATES) vc[mt][r] = live ? vc[mt][r] : 0.0f;  // (the padding is read by others)
+                    made(vc[mt][r]);
                 }
             if (c + 1 < nc) {
                 values(c + 1);
@@ -517,7 +526,7 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
                 }
             }
         }
-        if (M::TB == 1) wait_copies();  // (T and P of this chunk)
+        if (M::TB == 1) arrived();  // (T and P of this chunk)
         lds_barrier();
         if (c + 1 < nc && cw >= 0) {
             fetch_q(c + 1);
@@ -584,8 +593,7 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
                 for (int t = 0; t < 2 * DW; ++t) mma<NT, 3>(S[t], tfrag<NT, DS>(K, 2 * s0 + t, gp, lane), lt);
             }
         }
-        // the next chunk's operands have come; what is stored now has half a chunk's time to get out
-        wait_copies();
+        arrived();  // the next chunk's operands
         lds_barrier();
         if (c + 1 < nc && cw >= 0) {
             if (M::KB == 1) fetch_k(c + 1);
@@ -614,7 +622,7 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
             }
         }
         if (M::KB == 1 && c + 1 < nc) {
-            wait_copies();
+            arrived();
             lds_barrier();
         }
     }
