@@ -150,6 +150,21 @@ __device__ __forceinline__ Terms<NT> tfrag(const char *k, int t, int gp, int lan
     return r;
 }
 
+// use(i, load(i)) for i < N, with the loads AHEAD items before their use (0: where
+// the compiler likes, which is right before the products that wait for them).
+template <int N, int AHEAD, class Load, class Use>
+__device__ __forceinline__ void stream(Load load, Use use) {
+    decltype(load(0)) f[AHEAD + 1];
+#pragma unroll
+    for (int i = 0; i < AHEAD && i < N; ++i) f[i] = load(i);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (i + AHEAD < N) f[(i + AHEAD) % (AHEAD + 1)] = load(i + AHEAD);
+        if (AHEAD) asm volatile("" ::: "memory");
+        use(i, f[i % (AHEAD + 1)]);
+    }
+}
+
 // Sizes of a chunk's operands.  DS: groups of 32 of dk; MT: tiles of 16
 // samples.  Float inputs take chunks of 32 samples, so that their three terms
 // fit the LDS at dk = 256; bfloat16 ones take 64.

@@ -393,6 +393,13 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
     using F = Blob<E, DS, STATES>;
     using M = ScanLds<E, DS, KS, STATES>;
     constexpr int C = F::C, MT = F::MT, NT = F::NT, GP = F::GP, NP = F::NP, DW = DS / KS;
+    // Fragments in flight to the matrix cores.  A wave of up to two groups of dk has
+    // little else to do meanwhile (2048 samples of 8 memories of 128x64, bfloat16: 106 us,
+    // 111 with none); one of four, or that holds its part of Q, has no registers for them
+    // (4 x 4096 samples of 32 of 128x128: 418 us, 395 with none; 1024 of 16 of 256x256:
+    // 139 and 92).
+    constexpr bool ROOM = DW <= 2 && !M::DIRECT;
+    constexpr int AHEAD = !ROOM ? 0 : NT == 1 ? 3 : 1, AHEAD3 = ROOM ? 1 : 0;  // (of three terms)
     extern __shared__ char lds[];
     const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, gr = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), cw = wv - tiles * KS;  // cw >= 0: a copier
@@ -489,19 +496,24 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
             }
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) X[mt] = Y[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            constexpr int KQ = STATES || M::DIRECT ? 1 : 2;  // K alone, or K and Q in turn
+            Terms<3> st;
+            Terms<NP> sp;
+            stream<DW * MT * KQ, AHEAD>(
+                [&](int i) {
+                    return frag<NT>((i % KQ ? Q : K) + (i / KQ % MT * DS + s0 + i / KQ / MT) * NT * FRAG, lane);
+                },
+                [&](int i, const Terms<NT> &f) {
+                    const int s = i / KQ / MT, mt = i / KQ % MT;
+                    if (i % (KQ * MT) == 0) {
+                        st = split<3>(S[2 * s], S[2 * s + 1]);
 #pragma unroll
-            for (int s = 0; s < DW; ++s) {
-                const Terms<3> st = split<3>(S[2 * s], S[2 * s + 1]);
-                Terms<NP> sp;
-#pragma unroll
-                for (int i = 0; i < NP; ++i) sp.t[i] = st.t[i];
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    mma<NT, 3>(X[mt], frag<NT>(K + (mt * DS + s0 + s) * NT * FRAG, lane), st);
+                        for (int x = 0; x < NP; ++x) sp.t[x] = st.t[x];
+                    }
+                    if (i % KQ) mma<NT, NP>(Y[mt], f, sp);
+                    else mma<NT, 3>(X[mt], f, st);
                     if (M::DIRECT) mma<NT, NP>(Y[mt], qd[M::DIRECT ? s : 0][mt], sp);
-                    else if (!STATES) mma<NT, NP>(Y[mt], frag<NT>(Q + (mt * DS + s0 + s) * NT * FRAG, lane), sp);
-                }
-            }
+                });
             // the wave's own loads go out before the copies take the CU's path to memory
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
@@ -555,12 +567,14 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
                 for (int r = 0; r < 4; ++r) X[mt][r] = be[r] * (vc[mt][r] - ev[r] * X[mt][r]);
                 U[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
             }
-#pragma unroll
-            for (int gp = 0; gp < GP; ++gp) {
-                const Terms<3> rt = split<3>(X[2 * gp], X[2 * gp + 1]);
-#pragma unroll
-                for (int mt = 2 * gp; mt < MT; ++mt) mma<3, 3>(U[mt], frag<3>(T + F::lower(mt, gp) * 3 * FRAG, lane), rt);
-            }
+            Terms<3> rt;
+            stream<F::TRI, AHEAD3>(  // columns of 32 samples, below the diagonal
+                [&](int i) { return frag<3>(T + F::lower(i < MT ? i : i - MT + 2, i < MT ? 0 : 1) * 3 * FRAG, lane); },
+                [&](int i, const Terms<3> &f) {
+                    const int gp = i < MT ? 0 : 1, mt = i < MT ? i : i - MT + 2;
+                    if (mt == 2 * gp) rt = split<3>(X[2 * gp], X[2 * gp + 1]);
+                    mma<3, 3>(U[mt], f, rt);
+                });
             if (!STATES) {  // out
                 const char *yb = lds + M::AT_Y + tile * MT * (KS - 1) * FRAG;
                 Terms<NP> ut[GP];
@@ -584,14 +598,17 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
             const float end = co[C - 1];  // E of the last sample
 #pragma unroll
             for (int t = 0; t < 2 * DW; ++t) S[t] *= end;
-#pragma unroll
-            for (int gp = 0; gp < GP; ++gp) {
-                const f32x4 l0 = *reinterpret_cast<const f32x4 *>(co + 2 * C + 32 * gp + 4 * gr);
-                const f32x4 l1 = *reinterpret_cast<const f32x4 *>(co + 2 * C + 32 * gp + 16 + 4 * gr);
-                const Terms<3> lt = split<3>(U[2 * gp] * l0, U[2 * gp + 1] * l1);
-#pragma unroll
-                for (int t = 0; t < 2 * DW; ++t) mma<NT, 3>(S[t], tfrag<NT, DS>(K, 2 * s0 + t, gp, lane), lt);
-            }
+            Terms<3> lt;
+            stream<GP * 2 * DW, AHEAD>([&](int i) { return tfrag<NT, DS>(K, 2 * s0 + i % (2 * DW), i / (2 * DW), lane); },
+                                       [&](int i, const Terms<NT> &f) {
+                                           const int gp = i / (2 * DW), t = i % (2 * DW);
+                                           if (t == 0) {
+                                               const float *l = co + 2 * C + 32 * gp + 4 * gr;
+                                               lt = split<3>(U[2 * gp] * *reinterpret_cast<const f32x4 *>(l),
+                                                             U[2 * gp + 1] * *reinterpret_cast<const f32x4 *>(l + 16));
+                                           }
+                                           mma<NT, 3>(S[t], f, lt);
+                                       });
         }
         arrived();  // the next chunk's operands
         lds_barrier();
