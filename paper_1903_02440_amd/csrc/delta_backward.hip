@@ -48,6 +48,8 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
     using F = Blob<E, DS, true>;
     using M = RscanLds<E, DS, KS>;
     constexpr int C = F::C, MT = F::MT, NT = F::NT, GP = F::GP, DW = DS / KS;
+    constexpr bool ROOM = DW <= 2;
+    constexpr int AHEAD = !ROOM ? 0 : NT == 1 ? 3 : 1, AHEAD3 = ROOM ? 1 : 0;
     extern __shared__ char lds[];
     const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, gr = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
@@ -116,12 +118,13 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
             for (int t = 0; t < 2 * DW; ++t) at(dst + t * vgs * KEPT_BLOCK, lkept) = quad_transpose(S[t], lane);
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) X[mt] = Y[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int s = 0; s < DW; ++s) {
-                const Terms<3> st = split<3>(S[2 * s], S[2 * s + 1]);
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) mma<NT, 3>(X[mt], frag<NT>(K + (mt * DS + s0 + s) * NT * FRAG, lane), st);
-            }
+            Terms<3> st;
+            stream<DW * MT, AHEAD>([&](int i) { return frag<NT>(K + (i % MT * DS + s0 + i / MT) * NT * FRAG, lane); },
+                                   [&](int i, const Terms<NT> &f) {
+                                       const int s = i / MT;
+                                       if (i % MT == 0) st = split<3>(S[2 * s], S[2 * s + 1]);
+                                       mma<NT, 3>(X[i % MT], f, st);
+                                   });
             if (KS > 1) {
                 char *xb = lds + M::AT_X + tile * KS * MT * FRAG;
 #pragma unroll
@@ -159,21 +162,29 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)  // dU: last (K dS), and P^T dO on top
                 X[mt] *= *reinterpret_cast<const f32x4 *>(co + 2 * C + 16 * mt + 4 * gr);
+            // fragments of P^T, then of T^T: columns of 32 samples, above the diagonal
+            Terms<NT> ot;
+            Terms<3> ut;
+            stream<2 * F::TRI, AHEAD3>(
+                [&](int i) {
+                    const int f = i % F::TRI, gp = f < 2 ? 0 : 1, mt = f < 2 ? f : f - 2;
+                    return frag<3>((i < F::TRI ? PT : TT) + F::upper(mt, gp) * 3 * FRAG, lane);
+                },
+                [&](int i, const Terms<3> &fr) {
+                    const int f = i % F::TRI, gp = f < 2 ? 0 : 1, mt = f < 2 ? f : f - 2;
+                    if (i < F::TRI) {
+                        if (mt == 0) {
+                            float x[8];
 #pragma unroll
-            for (int gp = 0; gp < GP; ++gp) {
-                float x[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = o[2 * gp + (j >> 2)][j & 3];
-                const Terms<NT> ot = split<NT>(x);
-#pragma unroll
-                for (int mt = 0; mt <= 2 * gp + 1; ++mt) mma<3, NT>(X[mt], frag<3>(PT + F::upper(mt, gp) * 3 * FRAG, lane), ot);
-            }
-#pragma unroll
-            for (int gp = 0; gp < GP; ++gp) {
-                const Terms<3> ut = split<3>(X[2 * gp], X[2 * gp + 1]);
-#pragma unroll
-                for (int mt = 0; mt <= 2 * gp + 1; ++mt) mma<3, 3>(Y[mt], frag<3>(TT + F::upper(mt, gp) * 3 * FRAG, lane), ut);
-            }
+                            for (int j = 0; j < 8; ++j) x[j] = o[2 * gp + (j >> 2)][j & 3];
+                            ot = split<NT>(x);
+                        }
+                        mma<3, NT>(X[mt], fr, ot);
+                    } else {
+                        if (mt == 0) ut = split<3>(X[2 * gp], X[2 * gp + 1]);
+                        mma<3, 3>(Y[mt], fr, ut);
+                    }
+                });
             const float end = co[C - 1];
 #pragma unroll
             for (int t = 0; t < 2 * DW; ++t) S[t] *= end;
@@ -192,11 +203,8 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
                     }
                 }
                 const Terms<3> xt = split<3>(x), yt = split<3>(y);
-#pragma unroll
-                for (int t = 0; t < 2 * DW; ++t) {
-                    mma<NT, 3>(S[t], tfrag<NT, DS>(Q, 2 * s0 + t, gp, lane), xt);
-                    mma<NT, 3>(S[t], tfrag<NT, DS>(K, 2 * s0 + t, gp, lane), yt);
-                }
+                stream<4 * DW, AHEAD>([&](int i) { return tfrag<NT, DS>(i & 1 ? K : Q, 2 * s0 + i / 2, gp, lane); },
+                                      [&](int i, const Terms<NT> &f) { mma<NT, 3>(S[i / 2], f, i & 1 ? yt : xt); });
             }
         }
         wait_copies();
