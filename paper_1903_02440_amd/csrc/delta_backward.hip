@@ -113,9 +113,6 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
         const float *co = reinterpret_cast<const float *>(H);
         f32x4 X[MT], Y[MT];
         if (mine) {
-            f32x4 *dst = kept.dS + ((((int64_t)bh * w.NC + c) * 2 * DS + 2 * s0) * vgs + (ct >> 1)) * KEPT_BLOCK;
-#pragma unroll
-            for (int t = 0; t < 2 * DW; ++t) at(dst + t * vgs * KEPT_BLOCK, lkept) = quad_transpose(S[t], lane);
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) X[mt] = Y[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
             Terms<3> st;
@@ -185,6 +182,10 @@ __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out
                         mma<3, 3>(Y[mt], fr, ut);
                     }
                 });
+            // (here, so that they have the rest of the chunk to get out before a wait)
+            f32x4 *dst = kept.dS + ((((int64_t)bh * w.NC + c) * 2 * DS + 2 * s0) * vgs + (ct >> 1)) * KEPT_BLOCK;
+#pragma unroll
+            for (int t = 0; t < 2 * DW; ++t) at(dst + t * vgs * KEPT_BLOCK, lkept) = quad_transpose(S[t], lane);
             const float end = co[C - 1];
 #pragma unroll
             for (int t = 0; t < 2 * DW; ++t) S[t] *= end;
