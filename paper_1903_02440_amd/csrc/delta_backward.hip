@@ -38,9 +38,10 @@ struct RscanLds {
 
 // Grid, columns and parts as the states' kernel (delta_kernels.hpp), chunks from
 // last to first; the waves of a tile carry 16 columns of dS and add up K dS
-// through LDS.  All waves copy here: with some that only copy, the others have too
-// few registers (2 x 2048 samples of 32 memories of 128x128, bfloat16: 205 us, 190
-// without).  Bound as the states' kernel by a chunk's chain, 5.9 us.
+// through LDS.  All waves copy here: with some that only copied, the others had too
+// few registers (205 us against 190, before fragments were loaded ahead).  Bound as
+// the states' kernel by a chunk's chain, 4.9 us for 64 samples of 128x128 memories,
+// bfloat16 (2 x 2048 samples of 32 heads 158 us).
 template <class E, int DS, int KS>
 __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out, Args a,
                                                      const int32_t *__restrict__ lengths, int tiles, Chunks w,
@@ -311,10 +312,11 @@ struct GradLds {
 // order.  A wave owns 16 of the dk columns of dq, r and c (every eighth tile);
 // the sums over dv go by groups of 32 columns whose fragments all waves share,
 // and the tiles of M and N are dealt out among the waves.  The value heads of a
-// key head follow each other, so that their dq and dk add up in registers.  Six
-// terms' products of a float sum with another and their splits, with one workgroup
-// a CU (145 KB of LDS at 128 rows, bfloat16): waits take 59 % of the waves' time.
-// 2 x 2048 samples of 16 keys for 32 heads of 128x128: 310 us, 1.7 TB/s.
+// key head follow each other, so that their dq and dk add up in registers.  The LDS
+// (145 KB at 128 rows, bfloat16) leaves one workgroup a CU, whose eight waves wait for
+// each other between short steps: of a head of 128 columns four tenths of the time are
+// the sums over dv, a quarter the products with K and Q.  2 x 2048 samples of 16 keys
+// for 32 heads of 128x128: 236 us, 2.4 TB/s.
 template <class E, int DS, bool WIDE>
 __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
     const E *__restrict__ v, const float *__restrict__ g, const E *__restrict__ d_out, Args a,

@@ -340,9 +340,9 @@ __device__ __forceinline__ int head_of(int x, int n) { return n % 8 == 0 ? (x & 
 // copies go out at some 64 bytes a cycle and CU, and a wave that issues them
 // waits for that (2400 of 7100 cycles of a chunk of 250x10 memories, float, and
 // as much of 11000 of 128x128 ones, bfloat16).  1024 samples of 16 memories of
-// 128x128, float: 79 us with two such waves, 73 with four; 4 x 4096 samples of 32,
-// bfloat16: 425 us with two, 435 with four, 615 with eight, whose registers the
-// other waves lack.
+// 128x128, float: 75 us with two such waves, 73 with four or eight; 4 x 4096 samples of
+// 32, bfloat16: 395 us with two or four, 954 with eight, whose registers the other
+// waves lack.
 constexpr int COPIERS = 4;
 
 // Waves that carry columns, at most: those of one kernel are limited by their
@@ -382,9 +382,9 @@ struct ScanLds {
 // columns alone fill the SIMDs, more where they do not.  STATES: for the backward
 // pass, the state that enters each chunk and U are written instead of out (`kept`).
 // The chunks of a head follow each other: bound by a chunk's chain of products,
-// splits and two exchanges, 2.6 us for 32 samples of 250x10 memories, float (1000
-// samples 84 us), 5.0 us for 64 of 128x128, bfloat16 (4 x 4096 samples of 32 heads
-// 320 us, 160 TFLOP/s of the definition's products).
+// splits and two exchanges, 2.5 us for 32 samples of 250x10 memories, float (1000
+// samples 81 us), 4.3 us for 64 of 128x128, bfloat16 (4 x 4096 samples of 32 heads
+// 273 us, 190 TFLOP/s of the definition's products).
 template <class E, int DS, int KS, bool STATES>
 __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_scan(const E *__restrict__ v, Args a,
                                                     const int32_t *__restrict__ lengths, int tiles, Chunks w,
@@ -656,12 +656,12 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
 // How a call's columns go to waves: KS waves to a tile of 16 columns and `tiles`
 // of them a workgroup (`threads` in all), out of `all` tiles a head.  A CU's LDS
 // takes one workgroup, so more than 256 would wait for a second turn (8 ragged
-// sequences of 1531, 8 memories of 96x72, bfloat16: 114 us in 192 workgroups, 166 in 320).
+// sequences of 1531, 8 memories of 96x72, bfloat16: 107 us in 192 workgroups, 170 in 320).
 // Up to there a tile's sums over dk are shared by up to eight waves, while the
 // 1024 SIMDs have no more than one wave each (1000 samples of 8 memories of 250x10,
-// float: 103 us with eight, 175 with one; 2 x 1024 of 16 of 256x256, bfloat16: 117
-// with one, 108 with two, 117 with four), and tiles spread over more workgroups
-// (2048 samples of 8 memories of 128x64, bfloat16: 135 us with two tiles each, 112
+// float: 101 us with eight, 162 with one; 2 x 1024 of 16 of 256x256, bfloat16: 126
+// with one, 103 with two, 164 with four), and tiles spread over more workgroups
+// (2048 samples of 8 memories of 128x64, bfloat16: 131 us with two tiles each, 106
 // with one).
 struct Cols {
     int KS, tiles, blocks, threads;

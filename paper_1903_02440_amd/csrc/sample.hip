@@ -13,9 +13,10 @@
 // boundary's bin; sums by index; the draw), each reading the row again; where top_k
 // keeps few, the list holds all that matters and the last two are one launch of
 // a workgroup a row.  256 rows of 200003 floats: 33 us to read for the largest (6.2
-// TB/s, half of it from the cache behind HBM), 61 for the histogram of weights (some
-// 36 instructions a score), 39 for the list, 55 for the sums, 14 for the draw.  A row of 131072
-// bfloat16 scores, top_k 50: 4 + 5 + 8 + 10 us, the latency of four dependent steps.
+// TB/s, in part from the cache behind HBM), 67 for the histogram of weights (some 36
+// instructions a score), 37 for the list, 46 for the sums, 20 for the draw.  A row of
+// 131072 bfloat16 scores, top_k 50: 4 + 5 + 8 + 10 us, the latency of four dependent
+// steps.
 #include <algorithm>
 #include <cmath>
 
