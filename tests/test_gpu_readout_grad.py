@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import readout_ref as ref
-from test_gpu_readout import BF16, F32, make, seeded
+from test_gpu_readout import BF16, F32, close as near, make, seeded, size_of
 
 spk = pytest.importorskip("paper_1903_02440_amd")
 
@@ -159,3 +159,53 @@ def test_gradients_unaligned():
     for name, p, r, w in zip(("d_q", "d_k", "d_v", "d_g", "d_beta", "d_state"), a, b, want):
         close(p, w, 64, 32, 67, name)
         close(r, w, 64, 32, 67, name)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("dk", [20, 64, 128, 250])
+@pytest.mark.parametrize("B,dv", [(65, 40), (30, 40), (50, 10), (25, 10)])
+def test_many_memories(B, dv, dk, dtype):
+    """Enough heads that a tile of columns has fewer waves, and workgroups several tiles; the results of a few
+    sequences, padded ones among them, against the definition on them alone."""
+    L, Hk, Hv, some = 70, 2, 4, [0, 1, B // 2, B - 1]
+    x, s0 = make(B, L, Hk, Hv, dk, dv, dtype, 91)
+    d_out, d_last = upstream(x, s0)
+    lens = torch.full((B,), L, dtype=torch.int32)
+    lens[1], lens[B // 2] = 0, 33
+    out, last = spk.spk_delta_rule(**x, initial_state=s0, lengths=lens.cuda())
+    got = spk.spk_delta_rule_backward(*(x[n] for n in NAMES), d_out, d_final_state=d_last, initial_state=s0,
+                                      lengths=lens.cuda())
+    few = {n: t[some].contiguous() for n, t in x.items()}
+    want, final = ref.delta_rule(**few, scale=1.0, state=s0[some], lengths=lens[some])
+    m = size_of(few, s0[some], final)
+    near(out[some], want, dk, L, dtype, m, "out")
+    near(last[some], final, dk, L, F32, m, "state")
+    grads = reference(few, s0[some], 1.0, lens[some], d_out[some], d_last[some])
+    for name, a, b in zip(("d_q", "d_k", "d_v", "d_g", "d_beta", "d_state"), got, grads):
+        close(a[some], b, dk, dv, L, name)
+    assert all(bool(torch.isfinite(t).all()) for t in (out, last, *got))
+
+
+def test_offsets_beyond_32_bits():
+    """The last sequence (row) of a call whose tensors hold more than 2^32 (2^31) elements, as alone."""
+    r = torch.Generator(device="cuda").manual_seed(5)
+    B, L, Hv, dk, dv = 2, 33000, 16, 16, 4096
+    k = torch.nn.functional.normalize(torch.randn(B, L, 1, dk, generator=r, device="cuda"), dim=-1).to(BF16)
+    v = torch.randn(B, L, Hv, dv, generator=r, device="cuda", dtype=BF16)
+    g, beta = -torch.rand(B, L, Hv, generator=r, device="cuda"), torch.rand(B, L, Hv, generator=r, device="cuda")
+    assert v.numel() > 2 ** 32
+    out, last = spk.spk_delta_rule(k, k, v, g, beta)
+    alone = spk.spk_delta_rule(k[1:], k[1:], v[1:], g[1:], beta[1:])
+    assert torch.equal(out[1:], alone[0]) and torch.equal(last[1:], alone[1])
+    grads = spk.spk_delta_rule_backward(k, k, v, g, beta, out, d_initial_state=False)
+    alone = spk.spk_delta_rule_backward(k[1:], k[1:], v[1:], g[1:], beta[1:], out[1:], d_initial_state=False)
+    assert all(torch.equal(a[1:], b) for a, b in zip(grads[:5], alone[:5]))
+    del v, out, grads, alone
+    x = torch.randn(130, 1 << 24, 1, 1, generator=r, device="cuda", dtype=BF16)
+    u = torch.rand(130, generator=r, device="cuda")
+    assert x.numel() > 2 ** 31
+    for kw in (dict(top_p=0.5), dict(top_k=40)):
+        w, n = spk.spk_sample_winners(x, u, **kw)
+        w1, _ = spk.spk_sample_winners(x[129:], u[129:], **kw)
+        assert torch.equal(w[129:], w1) and bool((n == 1).all())
+    torch.cuda.empty_cache()
