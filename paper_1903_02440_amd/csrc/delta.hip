@@ -188,9 +188,9 @@ void launch_seq(const void *q, const void *k, const void *v, const float *g, con
 }
 
 // A call of more samples goes in chunks: below, two launches and a whole chunk's
-// products cost more than going sample by sample.  8 x 250x10 memories, float: 14.0 us
-// against 17.9 in chunks for 8 samples, 18.8 against 18.5 for 12; 512 x 128x128,
-// bfloat16: 44.6 against 55.8 for 8, 61.4 against 55.6 for 12.
+// products cost more than going sample by sample.  8 x 250x10 memories, float: 14.9 us
+// against 17.5 in chunks for 8 samples, 18.8 against 18.3 for 12; 512 x 128x128,
+// bfloat16: 45 against 51 for 8, 55 against 51 for 10.
 bool in_chunks(const Args &a) { return a.L > 10; }
 
 }  // namespace

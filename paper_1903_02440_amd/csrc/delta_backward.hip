@@ -38,10 +38,10 @@ struct RscanLds {
 
 // Grid, columns and parts as the states' kernel (delta_kernels.hpp), chunks from
 // last to first; the waves of a tile carry 16 columns of dS and add up K dS
-// through LDS.  All waves copy here: with some that only copied, the others had too
-// few registers (205 us against 190, before fragments were loaded ahead).  Bound as
-// the states' kernel by a chunk's chain, 4.9 us for 64 samples of 128x128 memories,
-// bfloat16 (2 x 2048 samples of 32 heads 158 us).
+// through LDS.  All waves copy here: with some that only copy the others have fewer
+// registers, and the time is the same (all gradients of 2 x 1024 samples of 32 memories
+// of 128x128, bfloat16: 265 and 266 us).  Bound as the states' kernel by a chunk's
+// chain, 4.9 us for 64 of those samples (2 x 2048: 158 us).
 template <class E, int DS, int KS>
 __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out, Args a,
                                                      const int32_t *__restrict__ lengths, int tiles, Chunks w,
