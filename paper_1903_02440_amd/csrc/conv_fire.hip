@@ -73,9 +73,10 @@ constexpr int NTILE_ALIGN = 4;  // the N tiles (16 features) are padded to a mul
 // Issued as inline assembly so that the compiler, which cannot tell which LDS
 // bytes the transfer writes, does not wait for it before every later LDS read;
 // the caller waits for it explicitly (vmcnt) before the barrier that hands the
-// buffer to the other waves.
+// buffer to the other waves.  The wait state between the write of m0 and the copy
+// is in the statement: the compiler adds none for an instruction of inline assembly.
 __device__ __forceinline__ void lds_dma16(const uint4 *gsrc, uint32_t m0) {
-    asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(gsrc), "{m0}"(m0) : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(gsrc), "{m0}"(m0) : "memory");
 }
 
 // A workgroup barrier for LDS hand-offs only: this wave's LDS operations

@@ -205,11 +205,12 @@ __device__ __forceinline__ double log_decay(float g) { return g < -1e4f ? -1e4 :
 // 16-byte aligned.  All waves of the workgroup take part.  The copy is one the
 // compiler does not count: before use, wait for vmcnt(0) and then a barrier.
 // (As a builtin it would make every LDS read wait for it, also those of another
-// buffer.)
+// buffer.)  The wait state that a copy needs after a write of m0 is in the statement:
+// the compiler adds none for an instruction of inline assembly.
 __device__ __forceinline__ void to_lds(char *dst, const char *src, int n, int wave, int waves, int lane) {
     const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)dst;
     for (int o = wave * FRAG; o < n; o += waves * FRAG)
-        asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(src + o + lane * 16),
+        asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src + o + lane * 16),
                      "{m0}"(__builtin_amdgcn_readfirstlane((int)(at + o)))
                      : "memory");
 }
