@@ -172,16 +172,15 @@ template <class E>
 struct Type;
 template <>
 struct Type<float> {
-    static constexpr int NT = 3, MT = 2, NP = 3;
+    static constexpr int NT = 3, MT = 2;
 };
 template <>
 struct Type<uint16_t> {
-    // the products that only reach a bfloat16 output take two terms (2^-17)
-    static constexpr int NT = 1, MT = 4, NP = 2;
+    static constexpr int NT = 1, MT = 4;
 };
 template <class E, int DS>
 struct Lay {
-    static constexpr int NT = Type<E>::NT, MT = Type<E>::MT, NP = Type<E>::NP;
+    static constexpr int NT = Type<E>::NT, MT = Type<E>::MT;
     static constexpr int C = 16 * MT, GP = MT / 2;
     // a triangular C x C operand: the fragments that are not zero throughout
     static constexpr int TRI = MT == 4 ? 6 : 2;

@@ -16,9 +16,8 @@ constexpr int LDS_BYTES = 160 * 1024;
 template <class E, int DS, bool BWD>
 struct Blob : Lay<E, DS> {
     using B = Lay<E, DS>;
-    static constexpr int NP = BWD ? 3 : B::NP;
     static constexpr int KEY = 2 * B::K;
-    static constexpr int T = B::TRI * 3 * FRAG, P = B::TRI * NP * FRAG;
+    static constexpr int T = B::TRI * 3 * FRAG, P = T;
     static constexpr int TTAT = T + B::COEF, PAT = TTAT + (BWD ? T : 0);
     static constexpr int HEAD = PAT + P;
 };
@@ -266,7 +265,7 @@ __global__ __launch_bounds__(PREP_THREADS, 4) void k_delta_prep(const E *__restr
                 const float p = T[hi * PITCH + lo];
                 x[j] = lo <= hi ? p : 0.0f;
             }
-            put_frag<F::NP>(head + F::PAT + f * F::NP * FRAG, lane, split<F::NP>(x));
+            put_frag<3>(head + F::PAT + f * 3 * FRAG, lane, split<3>(x));
         }
         float x[16];
         if (wv < MT) {  // diagonal block wv, column m (all lane groups alike)
@@ -355,8 +354,8 @@ constexpr int carriers() {
 // LDS of the states' kernel, for KS waves to a tile of 16 columns.  K is needed all
 // through a chunk and has two buffers where they fit; T, the coefficients and P from
 // the middle on, with two where those still fit; Q is done with in the middle and
-// has one, or none (DIRECT) where K's second only fits without it and a wave has
-// registers for its own part of Q.  Then the partial sums that the waves of a tile
+// has one, or none (DIRECT) where K's second, or even its first, only fits without it
+// and a wave has registers for its own part of Q.  Then the partial sums that the waves of a tile
 // exchange.
 template <class E, int DS, int KS, bool STATES>
 struct ScanLds {
@@ -364,8 +363,7 @@ struct ScanLds {
     static constexpr int TP = STATES ? F::T + F::COEF : F::HEAD, TILES = carriers<DS, KS>() / KS;
     static constexpr int X = KS > 1 ? carriers<DS, KS>() * F::MT * FRAG : 0;
     static constexpr int Y = STATES ? 0 : TILES * F::MT * (KS - 1) * FRAG;
-    static constexpr bool DIRECT = !STATES && F::MT * (DS / KS) * F::NT <= 12 && 3 * F::K + TP + X + Y > LDS_BYTES &&
-                                   2 * F::K + TP + X + Y <= LDS_BYTES;
+    static constexpr bool DIRECT = !STATES && F::MT * (DS / KS) * F::NT <= 12 && 3 * F::K + TP + X + Y > LDS_BYTES;
     static constexpr int Q = STATES || DIRECT ? 0 : F::K;
     static constexpr int KB = 2 * F::K + Q + TP + X + Y <= LDS_BYTES ? 2 : 1;
     static constexpr int TB = KB * F::K + Q + 2 * TP + X + Y <= LDS_BYTES ? 2 : 1;
@@ -392,7 +390,7 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
                                                     Kept kept) {
     using F = Blob<E, DS, STATES>;
     using M = ScanLds<E, DS, KS, STATES>;
-    constexpr int C = F::C, MT = F::MT, NT = F::NT, GP = F::GP, NP = F::NP, DW = DS / KS;
+    constexpr int C = F::C, MT = F::MT, NT = F::NT, GP = F::GP, DW = DS / KS;
     // Fragments in flight to the matrix cores.  A wave of up to two groups of dk has
     // little else to do meanwhile (2048 samples of 8 memories of 128x64, bfloat16: 106 us,
     // 111 with none); one of four, or that holds its part of Q, has no registers for them
@@ -498,21 +496,15 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
             for (int mt = 0; mt < MT; ++mt) X[mt] = Y[mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
             constexpr int KQ = STATES || M::DIRECT ? 1 : 2;  // K alone, or K and Q in turn
             Terms<3> st;
-            Terms<NP> sp;
             stream<DW * MT * KQ, AHEAD>(
                 [&](int i) {
                     return frag<NT>((i % KQ ? Q : K) + (i / KQ % MT * DS + s0 + i / KQ / MT) * NT * FRAG, lane);
                 },
                 [&](int i, const Terms<NT> &f) {
                     const int s = i / KQ / MT, mt = i / KQ % MT;
-                    if (i % (KQ * MT) == 0) {
-                        st = split<3>(S[2 * s], S[2 * s + 1]);
-#pragma unroll
-                        for (int x = 0; x < NP; ++x) sp.t[x] = st.t[x];
-                    }
-                    if (i % KQ) mma<NT, NP>(Y[mt], f, sp);
-                    else mma<NT, 3>(X[mt], f, st);
-                    if (M::DIRECT) mma<NT, NP>(Y[mt], qd[M::DIRECT ? s : 0][mt], sp);
+                    if (i % (KQ * MT) == 0) st = split<3>(S[2 * s], S[2 * s + 1]);
+                    mma<NT, 3>(i % KQ ? Y[mt] : X[mt], f, st);
+                    if (M::DIRECT) mma<NT, 3>(Y[mt], qd[M::DIRECT ? s : 0][mt], st);
                 });
             // the wave's own loads go out before the copies take the CU's path to memory
 #pragma unroll
@@ -577,9 +569,9 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
                 });
             if (!STATES) {  // out
                 const char *yb = lds + M::AT_Y + tile * MT * (KS - 1) * FRAG;
-                Terms<NP> ut[GP];
+                Terms<3> ut[GP];
 #pragma unroll
-                for (int gp = 0; gp < GP; ++gp) ut[gp] = split<NP>(U[2 * gp], U[2 * gp + 1]);
+                for (int gp = 0; gp < GP; ++gp) ut[gp] = split<3>(U[2 * gp], U[2 * gp + 1]);
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {
                     if (part != mt * KS / MT) continue;
@@ -589,7 +581,7 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
                     Y[mt] *= *reinterpret_cast<const f32x4 *>(co + 3 * C + 16 * mt + 4 * gr);
 #pragma unroll
                     for (int gp = 0; gp <= mt / 2; ++gp)
-                        mma<NP, NP>(Y[mt], frag<NP>(P + F::lower(mt, gp) * NP * FRAG, lane), ut[gp]);
+                        mma<3, 3>(Y[mt], frag<3>(P + F::lower(mt, gp) * 3 * FRAG, lane), ut[gp]);
                 }
             } else {
 #pragma unroll
