@@ -427,9 +427,9 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
                 float x[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] = i0 < n && cv + j < a.dv ? vo.get(j) : 0.0f;
-                put_frag<3>((of_u ? fu : fy) + mt0 * 3 * FRAG, lane, split<3>(y));
+                put_frag<3>((of_u ? fu : fy) + mt0 * 3 * FRAG, lane, split<3, true>(y));
                 if (of_u) {
-                    put_frag<NT>(fo + mt0 * NT * FRAG, lane, split<NT>(x));
+                    put_frag<NT>(fo + mt0 * NT * FRAG, lane, split<NT, true>(x));
                 } else {
                     const float be = co[C + i0];
                     float d[8];

@@ -12,8 +12,8 @@
 //
 // Products run on the 16-bit matrix cores with float sums.  A float operand is
 // the exact sum of three bfloat16 terms (8 bits each), a bfloat16 input is one;
-// of a product of two such sums the terms below 2^-24 of the first are left
-// out.  Against the float matrix cores (1/16 of the rate) three or six products
+// of a product of two such sums the products of terms below 2^-22 of the whole are
+// left out.  Against the float matrix cores (1/16 of the rate) three or six products
 // of terms cost 3/16 to 6/16, at the same precision.
 //
 // Operands lie in fragments: for 16 rows and 32 summed indices the 16 bytes of
@@ -55,30 +55,36 @@ __device__ __forceinline__ uint32_t upper2(uint32_t lo, uint32_t hi) {
     return __builtin_amdgcn_perm(hi, lo, 0x07060302u);
 }
 
-// Eight floats as N bfloat16 terms.  Each term takes the leading 8 bits of what
-// is left (truncated, so that the remainder is exact): three hold every float.
-// The last term of a shorter sum is rounded to nearest.
-template <int N>
+// Eight floats as N bfloat16 terms: three hold every float.  Cut off, each term
+// takes the leading 8 bits of what is left; NEAREST, the first two are rounded, and
+// may have the other sign.  One operand of a product is to be NEAREST: the products
+// that mma() leaves out, of second and third terms, are then below 2^-22 of the whole,
+// without a preferred sign.  (Of two operands that are cut off it would be 2^-21, always
+// below the true product.)  It is the one made outside the passes over the chunks,
+// which are 2 to 5 % slower where they round.  A single term is rounded.
+template <int N, bool NEAREST = false>
 __device__ __forceinline__ Terms<N> split(const float (&x)[8]) {
+    constexpr float MOST = 3.38953139e38f;  // the largest bfloat16: rounding is not to reach infinity
     Terms<N> r;
     float y[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) y[j] = x[j];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        if (i == N - 1 && N < 3) {
+        const bool nearest = N == 1 || (NEAREST && i < 2);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                r.t[i][j] = (uint32_t)from_float<uint16_t>(y[2 * j]) |
-                            ((uint32_t)from_float<uint16_t>(y[2 * j + 1]) << 16);
-            break;
+        for (int j = 0; j < 4; ++j) {
+            const bool clamp = NEAREST && N == 3 && i == 0;
+            const float lo = clamp ? __builtin_amdgcn_fmed3f(y[2 * j], -MOST, MOST) : y[2 * j];
+            const float hi = clamp ? __builtin_amdgcn_fmed3f(y[2 * j + 1], -MOST, MOST) : y[2 * j + 1];
+            r.t[i][j] = nearest ? (uint32_t)from_float<uint16_t>(lo) | ((uint32_t)from_float<uint16_t>(hi) << 16)
+                                : upper2(__float_as_uint(lo), __float_as_uint(hi));
         }
+        if (i == N - 1) break;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            r.t[i][j] = upper2(__float_as_uint(y[2 * j]), __float_as_uint(y[2 * j + 1]));
-        if (i < N - 1) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] -= __uint_as_float(__float_as_uint(y[j]) & 0xFFFF0000u);
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t w = nearest ? r.t[i][j >> 1] : __float_as_uint(y[j]);
+            y[j] -= __uint_as_float(nearest && !(j & 1) ? w << 16 : w & 0xFFFF0000u);
         }
     }
     return r;

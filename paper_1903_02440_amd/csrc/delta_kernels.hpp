@@ -175,7 +175,7 @@ __global__ __launch_bounds__(PREP_THREADS, 4) void k_delta_prep(const E *__restr
                 const bool isq = f >= MT * DS;
                 float y[8];
                 as_floats(raw[x], s, gr, a.dk, 16 * mt + m < n, y);
-                const Terms<NT> t = split<NT>(y);
+                const Terms<NT> t = split<NT, true>(y);
                 const int o = (mt * DS + s) * NT * FRAG;
                 put_frag<NT>((isq ? fq : fk) + o, lane, t);
                 put_frag<NT>(key + (isq ? F::K : 0) + o, lane, t);
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(PREP_THREADS, 4) void k_delta_prep(const E *__restr
                 const float p = T[hi * PITCH + lo];
                 x[j] = lo <= hi ? p : 0.0f;
             }
-            put_frag<3>(head + F::PAT + f * 3 * FRAG, lane, split<3>(x));
+            put_frag<3>(head + F::PAT + f * 3 * FRAG, lane, split<3, true>(x));
         }
         float x[16];
         if (wv < MT) {  // diagonal block wv, column m (all lane groups alike)
@@ -325,7 +325,7 @@ __global__ __launch_bounds__(PREP_THREADS, 4) void k_delta_prep(const E *__restr
                 const float t = T[hi * PITCH + lo];
                 y[j] = lo <= hi ? t : 0.0f;
             }
-            put_frag<3>(head + (up ? F::TTAT : 0) + f * 3 * FRAG, lane, split<3>(y));
+            put_frag<3>(head + (up ? F::TTAT : 0) + f * 3 * FRAG, lane, split<3, true>(y));
         }
         if (hr + 1 < rep) __syncthreads();
     }

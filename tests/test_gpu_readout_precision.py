@@ -36,3 +36,44 @@ def test_what_was_stored_is_read_back_over_a_large_state(B, Hv, dk, dv, L, dtype
     assert bool((err <= tol + half * (want.abs() + tol)).all()), float((err - tol - half * want.abs()).max())
     err = (last.double().cpu() - final).abs()
     assert bool((err <= 16 * 2.0 ** -24 * (S.double().abs() + final.abs() + 8)).all())
+
+
+def worst():
+    """A number whose second and third bfloat16 terms are as large as they get when each is cut off, not rounded."""
+    return 1 + 2.0 ** -7 - 2.0 ** -23
+
+
+@pytest.mark.parametrize("dk", [1, 40, 200])
+def test_float_products(dk):
+    """beta = 0 and no decay: out_t = q_t . S, one product here, of floats held as sums of three bfloat16 terms.  The
+    products of terms that are made are exact, and adding them rounds: the sums before the last are below 2^-5 of
+    the product, so all roundings together are below 2^-23 of it; 2^-22 leaves as much again for products of terms
+    that are not made.  (Of terms that are cut off, not rounded, these are 2^-21 here.)"""
+    B, L, dv = 1, 40, 20
+    q = torch.zeros(B, L, 1, dk)
+    q[..., dk // 2] = worst()
+    S = torch.zeros(B, 1, dk, dv)
+    S[:, :, dk // 2] = worst() * 2.0 ** torch.arange(dv)
+    zero = torch.zeros(B, L, 1)
+    out, last = spk.spk_delta_rule(q.cuda(), q.cuda(), torch.zeros(B, L, 1, dv).cuda(), zero.cuda(), zero.cuda(),
+                                   initial_state=S.cuda())
+    want = (q.double() @ S.double()[:, 0]).reshape(out.shape)
+    assert bool(((out.double().cpu() - want).abs() <= 2.0 ** -22 * want).all())
+    assert torch.equal(last.cpu(), S)
+
+
+def test_float_values_up_to_the_largest():
+    """The terms of the largest floats are finite: the states and queries up to the type's end give finite products."""
+    B, L, dk, dv = 1, 33, 4, 5
+    q = torch.zeros(B, L, 1, dk)
+    q[:, :, :, 1] = torch.finfo(F32).max
+    k = torch.zeros(B, L, 1, dk)
+    k[..., 0] = 1.0
+    S = torch.full((B, 1, dk, dv), 2.0 ** -10)
+    S[:, :, 2] = torch.finfo(F32).max
+    zero = torch.zeros(B, L, 1)
+    out, last = spk.spk_delta_rule(q.cuda(), k.cuda(), torch.zeros(B, L, 1, dv).cuda(), zero.cuda(), zero.cuda(),
+                                   initial_state=S.cuda())
+    want = torch.full((B, L, 1, dv), torch.finfo(F32).max * 2.0 ** -10, dtype=torch.float64)
+    assert bool(((out.double().cpu() - want).abs() <= 2.0 ** -22 * want).all())
+    assert torch.equal(last.cpu(), S)
