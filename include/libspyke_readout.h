@@ -40,7 +40,14 @@ enum { SPK_F32 = 0, SPK_BF16 = 1 };
  * larger rates can grow without bound, as the rule does.
  *   q, k       dtype [B][L][Hk][dk]; value head h reads key head h / (Hv/Hk).
  *   v, out     dtype [B][L][Hv][dv].
- *   g, beta    f32 [B][L][Hv]; e^g must be finite (g = -inf forgets all).
+ *   g, beta    f32 [B][L][Hv]; g <= 0 (-inf forgets all).  A state may also
+ *              grow a little: the g above 0 of any 64 samples in a row may
+ *              add up to 1.  Where a call of more than 10 samples, or one for
+ *              gradients, finds more it makes what depends on those samples
+ *              NaN, in their sequence and head: the outputs from up to 63
+ *              samples before them on, the final state, the gradients (those
+ *              of q and k for the whole key head).  Up to 10 samples go one
+ *              by one and take any g whose e^g is finite.
  *   lengths    i32 [B] or NULL (all L): samples of each sequence, read as
  *              clamped to [0, L].  Rows of out behind a sequence's length are
  *              not written, and input rows behind it are not read.
@@ -64,7 +71,7 @@ SPK_API int spk_delta_rule(const void *q, const void *k, const void *v, const fl
  * a call per sample equals one spk_delta_rule call over them, up to rounding).
  *   q, k  dtype [B][Hk][dk]; v, out  dtype [B][Hv][dv]; g, beta  f32 [B][Hv];
  *   state f32 [B][Hv][dk][dv].
- * Limits as spk_delta_rule.  No workspace.                                  */
+ * Limits as spk_delta_rule, any g whose e^g is finite.  No workspace.                                  */
 SPK_API int spk_delta_rule_step(const void *q, const void *k, const void *v, const float *g, const float *beta,
                                 int dtype, int B, int Hk, int Hv, int dk, int dv, float scale, float *state, void *out,
                                 void *stream);

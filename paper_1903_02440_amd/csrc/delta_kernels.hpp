@@ -102,6 +102,13 @@ __device__ __forceinline__ void made(float &x) { asm volatile("" : "+v"(x) : : "
 
 constexpr int PREP_THREADS = 256;
 
+// Log decays above 0 may add up to this in a chunk.  A and P hold e^{gamma_i - gamma_j},
+// and T and the sums over a chunk cancel what these grow by where the rule itself
+// replaces it: their errors are the rule's times e to that sum (unit keys that repeat,
+// beta = 1, g = 1/4: no digit is left of 64 samples).  Beyond, the chunk's
+// decays become NaN, and with them all that the rule makes from it.
+constexpr float MAX_RISE = 1.0f;
+
 // triangular fragment f as (tile of rows, group of summed indices): the lower
 // ones of T and P, the upper ones of their transposes
 template <int MT, bool UP>
@@ -215,6 +222,12 @@ __global__ __launch_bounds__(PREP_THREADS, 4) void k_delta_prep(const E *__restr
                 for (int o = 1; o < C; o <<= 1) {
                     const double p = __shfl_up(s, o, 64);
                     if (lane >= o) s += p;
+                }
+                float rise = in && gv > 0.0f ? gv : 0.0f;
+                if (__ballot(rise > 0.0f)) {  // (uniform, and rare)
+#pragma unroll
+                    for (int o = 32; o >= 1; o >>= 1) rise += __shfl_xor(rise, o, 64);
+                    if (rise > MAX_RISE) s = NAN;
                 }
                 const double end = __shfl(s, C - 1, 64);
                 if (lane < C) {

@@ -118,7 +118,8 @@ def spk_delta_rule(q, k, v, g, beta, scale=1.0, initial_state=None, lengths=None
     """Gated delta rule over a batch of sequences: q, k [B,L,Hk,dk] and v [B,L,Hv,dv] of one dtype (float32 or
     bfloat16), g, beta f32 [B,L,Hv] -> (out [B,L,Hv,dv], final_state f32 [B,Hv,dk,dv] or None).  lengths i32 [B]
     gives each sequence's samples; rows of a given `out` behind them are left as they were, those of a new one
-    are 0.  final_state may be initial_state."""
+    are 0.  final_state may be initial_state.  g is a log decay, at most 0: calls of more than 10 samples answer the
+    growth of a state by more than e within 64 samples with NaN."""
     dt, B, L, Hk, Hv, dk, dv = _delta_args(q, k, v, g, beta, lengths, initial_state)
     dev = q.device
     out = _rows(out, v, q.dtype, lengths, "out")
@@ -160,8 +161,9 @@ def spk_delta_rule_step(q, k, v, g, beta, state, scale=1.0, out=None):
 def spk_delta_rule_backward(q, k, v, g, beta, d_out, d_final_state=None, scale=1.0, initial_state=None, lengths=None,
                             d_q=None, d_k=None, d_v=None, d_g=None, d_beta=None, d_initial_state=None, workspace=None):
     """Gradients of spk_delta_rule's (out, final_state) -> (d_q, d_k, d_v, d_g, d_beta, d_initial_state or None)
-    from d_out [B,L,Hv,dv] and d_final_state f32 [B,Hv,dk,dv] (None: zeros).  Rows behind a sequence's length as in
-    spk_delta_rule.  d_initial_state may be d_final_state."""
+    from d_out [B,L,Hv,dv] and d_final_state f32 [B,Hv,dk,dv] (None: zeros).  Rows behind a sequence's length are as in
+    spk_delta_rule, and so is growth (g above 0), for any number of samples.  d_initial_state may be
+    d_final_state."""
     dt, B, L, Hk, Hv, dk, dv = _delta_args(q, k, v, g, beta, lengths, initial_state)
     dev, f32, state = q.device, torch.float32, (B, Hv, dk, dv)
     _need(d_out, q.dtype, (B, L, Hv, dv), "d_out")
