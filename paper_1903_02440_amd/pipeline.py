@@ -62,6 +62,7 @@ from . import (pool_out_size, conv_out_size, spk_conv_fire, spk_conv_fire_first_
                spk_encode_latency, spk_encode_latency_workspace_size, spk_kwta, spk_kwta_workspace_size,
                spk_local_normalization, spk_pool, spk_pool_first_spike, spk_rank_latency, spk_rstdp, spk_stdp,
                spk_stdp_workspace_size, spk_sample_winners, spk_sample_winners_workspace_size)
+from .readout import check_draw
 
 
 def _is_conv(st):
@@ -147,6 +148,7 @@ class Chain:
             st, tf = self.stages[last], self.bufs[last]["tf"]
             if st.k != 1 or not math.isinf(st.thr):
                 raise ValueError("sample needs a last conv stage with k = 1 and the infinite threshold")
+            check_draw(T, *tf.shape[1:], **sample)
             ws_bytes = max(ws_bytes, spk_sample_winners_workspace_size(0, B, *tf.shape[1:]))
             self.uniform = torch.zeros((B,), dtype=f32, device=dev)
         self.workspace = torch.empty(max(ws_bytes, 256), dtype=u8, device=dev)

@@ -191,6 +191,12 @@ def spk_sample_winners_workspace_size(dtype, B, C, H, W) -> int:
     return int(_lib.spk_sample_winners_workspace_size(dtype, B, C, H, W))
 
 
+def check_draw(T, C, H, W, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """Raises what spk_sample_winners raises for these settings (a call of no images: nothing is enqueued)."""
+    _check(_lib.spk_sample_winners(None, SPK_F32, None, None, 0, T, C, H, W, temperature, top_k, top_p, min_p, None, None,
+                                   None, 0, None))
+
+
 @_with_stream
 def spk_sample_winners(scores, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, t_first=None, T=1, winners=None,
                        n_winners=None, workspace=None):
