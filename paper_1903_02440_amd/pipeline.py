@@ -151,6 +151,8 @@ class Chain:
             check_draw(T, *tf.shape[1:], **sample)
             ws_bytes = max(ws_bytes, spk_sample_winners_workspace_size(0, B, *tf.shape[1:]))
             self.uniform = torch.zeros((B,), dtype=f32, device=dev)
+            # whether a draw waits for its numbers (taking the largest needs none)
+            self.uniform_missing = self.sample.get("temperature", 1.0) > 0 and self.sample.get("top_k", 0) != 1
         self.workspace = torch.empty(max(ws_bytes, 256), dtype=u8, device=dev)
         self.labels = torch.zeros((B,), dtype=i32, device=dev)
         self.decision = torch.empty((B,), dtype=i32, device=dev)
@@ -202,6 +204,13 @@ class Chain:
         return st.a_plus, st.a_minus
 
     def set_input(self, image=None, wave=None, labels=None, uniform=None):
+        """Copies the batch's inputs into the chain's buffers, where they stay for the
+        steps to come.  uniform (f32 [B] in [0, 1)): the numbers of the draws with `sample`,
+        without which no winner is drawn."""
+        if uniform is not None and self.sample is None:
+            raise ValueError("uniform: numbers for a draw, in a chain without sample")
+        if uniform is not None and tuple(uniform.shape) != (self.B,):
+            raise ValueError(f"uniform: expected shape {(self.B,)}, got {tuple(uniform.shape)}")
         if image is not None:
             self.image.copy_(image)
         if wave is not None:
@@ -210,6 +219,7 @@ class Chain:
             self.labels.copy_(labels)
         if uniform is not None:
             self.uniform.copy_(uniform)
+            self.uniform_missing = False
 
     # ---------------------------------------------------------------- run
     def forward(self, stream=None, hook=None, early_learn=False):
@@ -217,6 +227,8 @@ class Chain:
         called right before (phase 0) and after (phase 1) each C-ABI call;
         names are "encode", "conv<i>", "kwta<i>" ("draw<i>" with sample), "pool<i>",
         "decide"."""
+        if self.sample is not None and self.uniform_missing:
+            raise ValueError("uniform: set_input(uniform=...) comes before the first draw")
         mark = hook or (lambda name, phase: None)
         main = stream if stream is not None else torch.cuda.current_stream()
         self._wait_pending(-1, main)
@@ -443,6 +455,7 @@ class OnlineTrainer:
         self.img_stage = torch.zeros((self.K, H, W), dtype=torch.uint8, device=dev)
         self.lab_stage = torch.zeros((self.K,), dtype=torch.int32, device=dev)
         self.uni_stage = torch.zeros((self.K,), dtype=torch.float32, device=dev) if sample is not None else None
+        self.draws = sample is not None and self.chain.uniform_missing
         self.graph = None
 
     def set_weights(self, weights):
@@ -461,7 +474,7 @@ class OnlineTrainer:
         self.chain.image.copy_(self.img_stage[j:j + 1])
         self.chain.labels.copy_(self.lab_stage[j:j + 1])
         if self.uni_stage is not None:
-            self.chain.uniform.copy_(self.uni_stage[j:j + 1])
+            self.chain.set_input(uniform=self.uni_stage[j:j + 1])
         self.chain.step()
 
     def _capture(self):
@@ -484,8 +497,15 @@ class OnlineTrainer:
     def run(self, images, labels=None, uniform=None):
         """Learn from images (u8 [N, H, W] on the device) in order; labels
         (i32 [N]) feed the decision of a reward-modulated last layer, and
-        uniform (f32 [N] in [0, 1)) the draw of its winner with `sample`."""
+        uniform (f32 [N] in [0, 1)) the draw of its winner with `sample`, and is
+        required there unless its settings take the largest."""
         N = images.shape[0]
+        if uniform is not None and self.uni_stage is None:
+            raise ValueError("uniform: numbers for a draw, in a trainer without sample")
+        if uniform is not None and tuple(uniform.shape) != (N,):
+            raise ValueError(f"uniform: expected shape {(N,)}, got {tuple(uniform.shape)}")
+        if N and uniform is None and self.draws:
+            raise ValueError("uniform: a draw needs a number for each image")
         i = 0
         while i < N:
             n = min(self.K, N - i)
