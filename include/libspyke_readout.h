@@ -120,8 +120,9 @@ SPK_API int spk_delta_rule_backward(const void *q, const void *k, const void *v,
  *             -1 where no neuron is eligible; n_winners i32 [B], 1 or 0 (the
  *             form spk_decide and spk_rstdp read).
  * w is held as a 64-bit fixed-point number with 62 - ceil(log2(C*H*W))
- * fraction bits (51 at most), to the nearest, so that sums do not depend on
- * their order: repeated calls give the same winners.
+ * fraction bits (51 at most), off by 1e-14 of itself and half a step at most,
+ * so that sums do not depend on their order: repeated calls give the same
+ * winners.
  * Limits: 0 <= temperature < inf, 0 <= top_k, 0 < top_p <= 1,
  * 0 <= min_p <= 1, 1 <= T <= 255, C*H*W <= 2^24, B <= 2^21 (65535
  * where C*H*W > 16384).

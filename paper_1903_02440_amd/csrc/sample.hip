@@ -67,11 +67,13 @@ constexpr int POW_BITS = 7, POW = 1 << POW_BITS;  // entries of the table of 2^(
 constexpr int BINS = 2048;  // bins of a row's first histogram
 constexpr int LIST = 4096;  // keys of one bin that LDS takes
 
-// Weights of a row: 2^shift exp((score - largest) / temperature), to the nearest
-// integer.  With y = shift + (score - largest) log2(e) / temperature rounded to
-// n + j / POW (by adding a number whose last place that is) and r what rounding
-// left, it is 2^n 2^(j / POW) 2^r with 2^r from its series: the first term left
-// out, (r ln 2)^5 / 120, is below 2e-15.  +infinity as the largest weighs 2^shift.
+// Weights of a row: 2^shift exp((score - largest) / temperature), as integers.  With
+// y = shift + (score - largest) log2(e) / temperature rounded to n + j / POW (by adding
+// a number whose last place that is) and r what rounding left, it is 2^n 2^(j / POW)
+// 2^r with 2^r from its series: the first term left out, (r ln 2)^5 / 120, is below
+// 2e-15.  That and the roundings of y (2^-48) and of 1 / temperature (51 * 2^-53) stay
+// below 1e-14 of the weight: eight steps of a weight near 2^51, less than one from
+// shift 46 down.  +infinity as the largest weighs 2^shift.
 struct Weigher {
     double top, per, shift_d;
     float ftop;
