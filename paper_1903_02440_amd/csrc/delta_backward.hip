@@ -298,14 +298,14 @@ struct GradLds {
     static constexpr int PITCH = B::C + 4, SQ = B::C * PITCH * 4;
     static constexpr int ONE = B::MT * (B::NT + 6) * FRAG;  // dO, Y, U of 32 columns
     static constexpr int TRI = B::TRI * 3 * FRAG;           // N, M, N^T, (beta M)^T: four of these
-    static constexpr int SUMS = (2 * GRAD_WAVES + 2) * B::C * 4 + GRAD_WAVES * 4;
+    static constexpr int SUMS = (2 * GRAD_WAVES + 1) * B::C * 4 + GRAD_WAVES * 4;
     // M and N as floats take the room of the staged columns
     static constexpr int TEMP = ONE > 2 * SQ ? ONE : 2 * SQ;
     // K and Q, all of their groups of 32 of dk where they fit, else those of one pass of the waves
     static constexpr bool WHOLE = TEMP + 2 * B::K + 4 * TRI + SUMS + 8192 <= LDS_BYTES;
     static constexpr int GROUPS = WHOLE ? DS : GRAD_WAVES / 2, K = B::MT * GROUPS * B::NT * FRAG, KQ = 2 * K;
     static constexpr int AT_KQ = TEMP, AT_TRI = AT_KQ + KQ, AT_SUMS = AT_TRI + 4 * TRI;
-    static constexpr int AT_GAM = AT_SUMS + (SUMS + 15) / 16 * 16, BYTES = AT_GAM + B::C * 8 + 4 * B::C * 4;
+    static constexpr int AT_GAM = AT_SUMS + (SUMS + 15) / 16 * 16, BYTES = AT_GAM + B::C * 8 + 3 * B::C * 4;
 };
 
 // Grid (chunk, b * Hk + key head): everything of the list above that has no
@@ -337,8 +337,8 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
     char *fo = lds, *fy = fo + MT * NT * FRAG, *fu = fy + MT * 3 * FRAG;
     float *sqM = reinterpret_cast<float *>(lds), *sqN = sqM + C * PITCH;
     char *tri = lds + G::AT_TRI;  // N, M, N^T, (beta M)^T
-    float *sums = reinterpret_cast<float *>(lds + G::AT_SUMS);  // [waves][2][C], then y.v, beta; then the ends
-    float *yv = sums + 2 * GRAD_WAVES * C, *ends = yv + 2 * C;
+    float *sums = reinterpret_cast<float *>(lds + G::AT_SUMS);  // [waves][2][C], then y.v; then the ends
+    float *yv = sums + 2 * GRAD_WAVES * C, *ends = yv + C;
     double *gam = reinterpret_cast<double *>(lds + G::AT_GAM);
     float *co = reinterpret_cast<float *>(gam + C);  // E, beta, last
     const char *key = w.key + ((int64_t)blockIdx.y * w.NC + chunk) * F::KEY;
