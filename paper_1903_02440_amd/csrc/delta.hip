@@ -50,7 +50,7 @@ using Cols = typename std::conditional<VW == 4, float4u, float1u>::type;
 // row, and writes only the columns that are its own.  Both sums over dk go through
 // the wave's shuffles and then LDS, with one barrier a sample (the LDS sums
 // alternate between two buffers).  One sample is bound by reading and writing the
-// states: 256 x 32 of 128x128 in 235 us, 4.6 TB/s (a copy reaches 4.9).
+// states: 256 x 32 of 128x128 in 230 us, 4.7 TB/s (a copy reaches 4.9).
 template <class E, int VW, int RT>
 __global__ __launch_bounds__(THREADS) void k_delta_seq(const E *__restrict__ q, const E *__restrict__ k,
                                                        const E *__restrict__ v, const float *__restrict__ g,
@@ -188,9 +188,9 @@ void launch_seq(const void *q, const void *k, const void *v, const float *g, con
 }
 
 // A call of more samples goes in chunks: below, two launches and a whole chunk's
-// products cost more than going sample by sample.  8 x 250x10 memories, float: 14.9 us
-// against 17.5 in chunks for 8 samples, 18.8 against 18.3 for 12; 512 x 128x128,
-// bfloat16: 45 against 51 for 8, 55 against 51 for 10.
+// products cost more than going sample by sample.  8 x 250x10 memories, float: 15.2 us
+// against 19.2 in chunks for 8 samples, 20.8 against 19.9 for 12; 512 x 128x128,
+// bfloat16: 46 against 56 for 8, 56 either way for 10, 65 against 56 for 12.
 bool in_chunks(const Args &a) { return a.L > 10; }
 
 }  // namespace

@@ -39,9 +39,9 @@ struct RscanLds {
 // Grid, columns and parts as the states' kernel (delta_kernels.hpp), chunks from
 // last to first; the waves of a tile carry 16 columns of dS and add up K dS
 // through LDS.  All waves copy here: with some that only copy the others have fewer
-// registers, and the time is the same (all gradients of 2 x 1024 samples of 32 memories
-// of 128x128, bfloat16: 265 and 266 us).  Bound as the states' kernel by a chunk's
-// chain, 4.9 us for 64 of those samples (2 x 2048: 158 us).
+// registers, and all gradients of 2 x 1024 samples of 32 memories of 128x128, bfloat16,
+// take the same time to 1 us in 265.  Bound as the states' kernel by a chunk's chain,
+// 4.7 us for 64 of those samples (2 x 2048: 151 us).
 template <class E, int DS, int KS>
 __global__ __launch_bounds__(512) void k_delta_rscan(const E *__restrict__ d_out, Args a,
                                                      const int32_t *__restrict__ lengths, int tiles, Chunks w,
@@ -313,10 +313,9 @@ struct GradLds {
 // the sums over dv go by groups of 32 columns whose fragments all waves share,
 // and the tiles of M and N are dealt out among the waves.  The value heads of a
 // key head follow each other, so that their dq and dk add up in registers.  The LDS
-// (145 KB at 128 rows, bfloat16) leaves one workgroup a CU, whose eight waves wait for
-// each other between short steps: of a head of 128 columns four tenths of the time are
-// the sums over dv, a quarter the products with K and Q.  2 x 2048 samples of 16 keys
-// for 32 heads of 128x128: 236 us, 2.4 TB/s.
+// (144 KB at 128 rows, bfloat16) leaves one workgroup a CU, whose eight waves wait for
+// each other between short steps: the matrix cores are busy 18 % of the time.
+// 2 x 2048 samples of 16 keys for 32 heads of 128x128: 225 us, 2.6 TB/s.
 template <class E, int DS, bool WIDE>
 __global__ __launch_bounds__(GRAD_THREADS) void k_delta_grads(
     const E *__restrict__ v, const float *__restrict__ g, const E *__restrict__ d_out, Args a,

@@ -143,7 +143,7 @@ struct PrepLds {
 // on the float matrix cores, a block column a wave.  The steps are short and
 // wait for each other, so the LDS is kept small enough for four workgroups a CU
 // (dk <= 128, bfloat16).  4 x 4096 samples of 16 keys for 32 heads of 128x128,
-// bfloat16: 150 us, 3.5 TB/s read and written (190 us with the products in LDS).
+// bfloat16: 159 us, 3.7 TB/s read and written (40 us more with the products in LDS).
 template <class E, int DS, bool BWD>
 __global__ __launch_bounds__(PREP_THREADS, 4) void k_delta_prep(const E *__restrict__ q, const E *__restrict__ k,
                                                                 const float *__restrict__ g,
@@ -348,13 +348,10 @@ __global__ __launch_bounds__(PREP_THREADS, 4) void k_delta_prep(const E *__restr
 // key head, which read the same operands, on one XCD's L2.
 __device__ __forceinline__ int head_of(int x, int n) { return n % 8 == 0 ? (x & 7) * (n >> 3) + (x >> 3) : x; }
 
-// Waves of a workgroup that only copy the next chunk's operands to LDS.  The
-// copies go out at some 64 bytes a cycle and CU, and a wave that issues them
-// waits for that (2400 of 7100 cycles of a chunk of 250x10 memories, float, and
-// as much of 11000 of 128x128 ones, bfloat16).  1024 samples of 16 memories of
-// 128x128, float: 75 us with two such waves, 73 with four or eight; 4 x 4096 samples of
-// 32, bfloat16: 395 us with two or four, 954 with eight, whose registers the other
-// waves lack.
+// Waves of a workgroup that only copy the next chunk's operands to LDS: a wave that
+// issues copies waits while they go out.  1024 samples of 16 memories of 128x128, float:
+// 79 us with two such waves, 73 with four or eight; 4 x 4096 samples of 32, bfloat16:
+// 442 us with two or four, 994 with eight, whose registers the other waves lack.
 constexpr int COPIERS = 4;
 
 // Waves that carry columns, at most: those of one kernel are limited by their
@@ -394,8 +391,9 @@ struct ScanLds {
 // pass, the state that enters each chunk and U are written instead of out (`kept`).
 // The chunks of a head follow each other: bound by a chunk's chain of products,
 // splits and two exchanges, 2.5 us for 32 samples of 250x10 memories, float (1000
-// samples 81 us), 4.3 us for 64 of 128x128, bfloat16 (4 x 4096 samples of 32 heads
-// 273 us, 190 TFLOP/s of the definition's products).
+// samples 80 us), 4.7 us for 64 of 128x128, bfloat16 (4 x 4096 samples of 32 heads
+// 298 us, 173 TFLOP/s of the definition's products; the matrix cores are busy a third
+// of the time).
 template <class E, int DS, int KS, bool STATES>
 __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_scan(const E *__restrict__ v, Args a,
                                                     const int32_t *__restrict__ lengths, int tiles, Chunks w,
@@ -405,10 +403,10 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
     using M = ScanLds<E, DS, KS, STATES>;
     constexpr int C = F::C, MT = F::MT, NT = F::NT, GP = F::GP, DW = DS / KS;
     // Fragments in flight to the matrix cores.  A wave of up to two groups of dk has
-    // little else to do meanwhile (2048 samples of 8 memories of 128x64, bfloat16: 106 us,
-    // 111 with none); one of four, or that holds its part of Q, has no registers for them
-    // (4 x 4096 samples of 32 of 128x128: 418 us, 395 with none; 1024 of 16 of 256x256:
-    // 139 and 92).
+    // little else to do meanwhile (2048 samples of 8 memories of 128x64, bfloat16: 103 us,
+    // 108 with none); one of four, or that holds its part of Q, has no registers for them
+    // (4 x 4096 samples of 32 of 128x128: 490 us, 442 with none; 1024 of 16 of 256x256:
+    // 140 and 97).
     constexpr bool ROOM = DW <= 2 && !M::DIRECT;
     constexpr int AHEAD = !ROOM ? 0 : NT == 1 ? 3 : 1, AHEAD3 = ROOM ? 1 : 0;  // (of three terms)
     extern __shared__ char lds[];
@@ -661,12 +659,12 @@ __global__ __launch_bounds__(64 * (carriers<DS, KS>() + COPIERS)) void k_delta_s
 // How a call's columns go to waves: KS waves to a tile of 16 columns and `tiles`
 // of them a workgroup (`threads` in all), out of `all` tiles a head.  A CU's LDS
 // takes one workgroup, so more than 256 would wait for a second turn (8 ragged
-// sequences of 1531, 8 memories of 96x72, bfloat16: 107 us in 192 workgroups, 170 in 320).
+// sequences of 1531, 8 memories of 96x72, bfloat16: 111 us in 192 workgroups, 183 in 320).
 // Up to there a tile's sums over dk are shared by up to eight waves, while the
 // 1024 SIMDs have no more than one wave each (1000 samples of 8 memories of 250x10,
-// float: 101 us with eight, 162 with one; 2 x 1024 of 16 of 256x256, bfloat16: 126
-// with one, 103 with two, 164 with four), and tiles spread over more workgroups
-// (2048 samples of 8 memories of 128x64, bfloat16: 131 us with two tiles each, 106
+// float: 102 us with eight, 163 with one; 2 x 1024 of 16 of 256x256, bfloat16: 131
+// with one, 112 with two, 128 with four), and tiles spread over more workgroups
+// (2048 samples of 8 memories of 128x64, bfloat16: 126 us with two tiles each, 103
 // with one).
 struct Cols {
     int KS, tiles, blocks, threads;

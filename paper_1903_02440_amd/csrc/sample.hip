@@ -12,8 +12,8 @@
 // launches of several workgroups a row (largest score; histogram; the keys of the
 // boundary's bin; sums by index; the draw), each reading the row again; where top_k
 // keeps few, the list holds all that matters and the last two are one launch of
-// a workgroup a row.  256 rows of 200003 floats: 33 us to read for the largest (6.2
-// TB/s, in part from the cache behind HBM), 67 for the histogram of weights (some 36
+// a workgroup a row.  256 rows of 200003 floats: 32 us to read for the largest (6.4
+// TB/s, in part from the cache behind HBM), 66 for the histogram of weights (36
 // instructions a score), 37 for the list, 46 for the sums, 20 for the draw.  A row of
 // 131072 bfloat16 scores, top_k 50: 4 + 5 + 8 + 10 us, the latency of four dependent
 // steps.
