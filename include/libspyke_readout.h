@@ -71,7 +71,7 @@ SPK_API int spk_delta_rule(const void *q, const void *k, const void *v, const fl
  * a call per sample equals one spk_delta_rule call over them, up to rounding).
  *   q, k  dtype [B][Hk][dk]; v, out  dtype [B][Hv][dv]; g, beta  f32 [B][Hv];
  *   state f32 [B][Hv][dk][dv].
- * Limits as spk_delta_rule, any g whose e^g is finite.  No workspace.                                  */
+ * Limits as spk_delta_rule; any g whose e^g is finite.  No workspace.       */
 SPK_API int spk_delta_rule_step(const void *q, const void *k, const void *v, const float *g, const float *beta,
                                 int dtype, int B, int Hk, int Hv, int dk, int dv, float scale, float *state, void *out,
                                 void *stream);

@@ -365,8 +365,8 @@ constexpr int carriers() {
 // through a chunk and has two buffers where they fit; T, the coefficients and P from
 // the middle on, with two where those still fit; Q is done with in the middle and
 // has one, or none (DIRECT) where K's second, or even its first, only fits without it
-// and a wave has registers for its own part of Q.  Then the partial sums that the waves of a tile
-// exchange.
+// and a wave has registers for its own part of Q.  Then the partial sums that the waves
+// of a tile exchange.
 template <class E, int DS, int KS, bool STATES>
 struct ScanLds {
     using F = Blob<E, DS, STATES>;
